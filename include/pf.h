@@ -304,6 +304,64 @@ int pf_ragged_attn_fwd_static(const pf_pool *pool, const pf_index *index,
                               const void *q, const void *k_cur, const void *v_cur, void *out,
                               int q_tokens, float softmax_scale, void *stream);
 
+/* ---- in front of the attention: queries and keys ---------------------------- */
+
+/*
+ * Rotary positions.  The first rot_dim channels of a head are rot_dim/2 pairs; pair i belongs to one axis (the first
+ * axis_pairs[0] pairs to axis 0 and so on: one axis for a line of tokens, three for frame, row and column) and is turned by
+ * position[axis] * turns[i] full turns.  Layouts: half (interleaved = 0): pair i = channels i and i + rot_dim/2;
+ * interleaved: channels 2i and 2i + 1.  Channels from rot_dim on are not turned.
+ * Filled by pf_rope_init; read on the host, during a call only.
+ */
+#define PF_ROPE_MAX_PAIRS 64
+#define PF_ROPE_SCALE_NONE          0
+#define PF_ROPE_SCALE_LINEAR        1   /* every position divided by factor */
+#define PF_ROPE_SCALE_BY_WAVELENGTH 2   /* pairs that turn at least fast_turns times over original_positions stay as they are,
+                                           those that turn at most slow_turns times are slowed down by factor, a ramp between */
+typedef struct pf_rope_scaling {
+  int32_t kind;                /* PF_ROPE_SCALE_* */
+  int32_t reserved;            /* must be 0 */
+  double factor;               /* >= 1 (not read by NONE) */
+  double original_positions;   /* BY_WAVELENGTH: context length that the model was trained on, > 0 */
+  double slow_turns, fast_turns;   /* BY_WAVELENGTH: 0 <= slow_turns < fast_turns */
+  double magnitude;            /* cosines and sines are multiplied by it; 0 = 1 */
+} pf_rope_scaling;
+typedef struct pf_rope {
+  int32_t head_dim;            /* 64 or 128 */
+  int32_t rot_dim;             /* channels turned, a multiple of 8; 0 = none */
+  int32_t interleaved;
+  int32_t n_axes;              /* 1 .. 3 */
+  int32_t axis_pairs[3];       /* their sum is rot_dim/2 */
+  float   magnitude;
+  double  turns[PF_ROPE_MAX_PAIRS];   /* full turns per position of every pair */
+} pf_rope;
+
+/* turns of pair m of an axis with n pairs = base^(-m/n) / (2 pi), scaled by `scaling` (NULL = not).  Host only. */
+int pf_rope_init(pf_rope *rope, int head_dim, int rot_dim, int interleaved, int n_axes, const int32_t *axis_pairs,
+                 double base, const pf_rope_scaling *scaling);
+
+/* One tensor of pf_qk_norm_rope: rows of n_heads heads per token. */
+typedef struct pf_rope_rows {
+  const void *x;               /* dev bf16, 16-byte aligned */
+  void *out;                   /* dev bf16, 16-byte aligned; may be x with the same layout, must not overlap x otherwise */
+  const void *weight;          /* dev bf16 [head_dim], 16-byte aligned, or NULL (= 1) */
+  int32_t n_heads;             /* 0 = this tensor is left out (all pointers NULL) */
+  int32_t reserved;            /* must be 0 */
+  pf_chunk_layout x_layout, out_layout;   /* both strides 0 = packed [n_heads][n_tokens][head_dim] */
+} pf_rope_rows;
+
+/*
+ * RMS norm of every head's row, then the rotation by the token's position, queries and keys in one launch:
+ *   y = x / sqrt(mean(x^2) + eps) * weight;  every pair of y turned as described at pf_rope
+ * fp32 arithmetic, angles in 64 bits, rounded once.  The results are what pf_ragged_attn_fwd_strided, pf_packed_attn_fwd
+ * and pf_cache_append_strided take.
+ *   positions  dev int32 [n_axes][n_tokens], any values; may be NULL when rot_dim is 0
+ *   eps        > 0; 0 = no norm (weights must be NULL then)
+ * q and k must not be NULL; one of them may have n_heads = 0.  n_tokens = 0 does nothing.
+ */
+int pf_qk_norm_rope(const pf_rope *rope, int n_tokens, const int32_t *positions, const pf_rope_rows *q,
+                    const pf_rope_rows *k, float eps, void *stream);
+
 /* ---- before the hot path: which head gets which policy -------------------- */
 
 /*

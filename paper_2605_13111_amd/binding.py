@@ -18,7 +18,7 @@ PF_SYNC_STRIDE = 32            # int32 words between the per-head counters of pf
 EXPORTS = ["pf_index_work_bytes", "pf_attn_workspace_bytes", "pf_selected_count", "pf_retained_count", "pf_plan_segments",
            "pf_pool_reset", "pf_cache_append", "pf_cache_append_strided", "pf_build_index", "pf_ragged_attn_fwd",
            "pf_ragged_attn_fwd_strided", "pf_classify_heads", "pf_status_string", "pf_set_tuning", "pf_index_status_dev", "pf_ragged_attn_fwd_static",
-           "pf_set_block_trace"]
+           "pf_set_block_trace", "pf_rope_init", "pf_qk_norm_rope"]
 
 
 class pf_head_policy(ctypes.Structure):
@@ -45,6 +45,25 @@ class pf_index(ctypes.Structure):
                 ("cu_seqlens", ctypes.c_void_p), ("work", ctypes.c_void_p), ("work_bytes", ctypes.c_size_t),
                 ("q_tokens", ctypes.c_int32), ("T_built", ctypes.c_int32), ("n_blocks", ctypes.c_int32),
                 ("n_partials", ctypes.c_int32), ("variant", ctypes.c_int32), ("longest_seg", ctypes.c_int32)]
+
+
+PF_ROPE_MAX_PAIRS = 64
+PF_ROPE_SCALINGS = {"none": 0, "linear": 1, "by_wavelength": 2}
+
+
+class pf_rope_scaling(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int32), ("reserved", ctypes.c_int32), ("factor", ctypes.c_double), ("original_positions", ctypes.c_double),
+                ("slow_turns", ctypes.c_double), ("fast_turns", ctypes.c_double), ("magnitude", ctypes.c_double)]
+
+
+class pf_rope(ctypes.Structure):
+    _fields_ = [("head_dim", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("n_axes", ctypes.c_int32),
+                ("axis_pairs", ctypes.c_int32 * 3), ("magnitude", ctypes.c_float), ("turns", ctypes.c_double * PF_ROPE_MAX_PAIRS)]
+
+
+class pf_rope_rows(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("out", ctypes.c_void_p), ("weight", ctypes.c_void_p), ("n_heads", ctypes.c_int32),
+                ("reserved", ctypes.c_int32), ("x_layout", pf_chunk_layout), ("out_layout", pf_chunk_layout)]
 
 
 _lib = None
@@ -86,6 +105,10 @@ def lib():
         L.pf_ragged_attn_fwd_static.argtypes = [P(pf_pool), P(pf_index), V, V, V, V, I, ctypes.c_float, V]
         L.pf_classify_heads.restype = I
         L.pf_classify_heads.argtypes = [V, I, I, I, ctypes.c_double, ctypes.c_double, V, V, V, V]
+        L.pf_rope_init.restype = I
+        L.pf_rope_init.argtypes = [P(pf_rope), I, I, I, I, P(ctypes.c_int32), ctypes.c_double, P(pf_rope_scaling)]
+        L.pf_qk_norm_rope.restype = I
+        L.pf_qk_norm_rope.argtypes = [P(pf_rope), I, V, P(pf_rope_rows), P(pf_rope_rows), ctypes.c_float, V]
         L.pf_set_block_trace.restype = I
         L.pf_set_block_trace.argtypes = [V, ctypes.c_size_t]
         L.pf_set_tuning.restype = I
@@ -325,6 +348,44 @@ def pf_ragged_attn_fwd_strided(pool, index, q, k_cur, v_cur, out, workspace, sof
                                             v_cur.data_ptr(), out.data_ptr(), shape[1], float(softmax_scale),
                                             _ptr(workspace), ws_bytes, ctypes.byref(lay), _stream(stream)),
            "pf_ragged_attn_fwd_strided")
+
+
+def make_rope(head_dim, rot_dim=None, interleaved=False, axis_pairs=None, base=10000.0, scaling="none", factor=1.0, original_positions=0.0,
+              slow_turns=1.0, fast_turns=32.0, magnitude=1.0):
+    """A model's rotary positions as a ``pf_rope`` struct.  rot_dim: channels turned (default: all); axis_pairs: channel pairs of every
+    position axis (default: one axis); scaling: "none", "linear" or "by_wavelength"."""
+    rot_dim = head_dim if rot_dim is None else int(rot_dim)
+    pairs = [rot_dim // 2] if axis_pairs is None else [int(p) for p in axis_pairs]
+    rope = pf_rope()
+    sc = pf_rope_scaling(PF_ROPE_SCALINGS[scaling], 0, float(factor), float(original_positions), float(slow_turns), float(fast_turns), float(magnitude))
+    _check(lib().pf_rope_init(ctypes.byref(rope), int(head_dim), rot_dim, int(bool(interleaved)), len(pairs),
+                              (ctypes.c_int32 * max(1, len(pairs)))(*pairs), float(base), ctypes.byref(sc)), "pf_rope_init")
+    return rope
+
+
+def _rope_rows(rope, n_tokens, x, out, weight):
+    """A tensor and its result as a ``pf_rope_rows`` struct: bf16 views of logical shape [heads, tokens, head_dim]."""
+    if x is None:
+        assert out is None and weight is None
+        return pf_rope_rows()
+    shape, xs, os_ = x.shape, x.stride(), out.stride()
+    assert x.dtype is _BF16 and out.dtype is _BF16 and out.shape == shape and shape[1:] == (n_tokens, rope.head_dim)
+    assert xs[2] == 1 and os_[2] == 1
+    if weight is not None:
+        assert weight.dtype is _BF16 and weight.shape == (rope.head_dim,) and weight.is_contiguous()
+    return pf_rope_rows(x.data_ptr(), out.data_ptr(), _ptr(weight), shape[0], 0, pf_chunk_layout(xs[1], xs[0]), pf_chunk_layout(os_[1], os_[0]))
+
+
+def pf_qk_norm_rope(rope, positions, q, q_out, k=None, k_out=None, q_weight=None, k_weight=None, eps=0.0, stream=None):
+    """RMS norm per head (eps > 0) and rotation of queries and keys in one launch.  q, k, q_out, k_out: bf16 views of logical shape [heads,
+    tokens, head_dim], e.g. [tokens, heads, head_dim] tensors seen heads first; q_out may be q.  Either pair may be None.  positions: int32
+    [axes, tokens], contiguous."""
+    n_tokens = (k if q is None else q).shape[1]
+    if rope.rot_dim:
+        assert positions.dtype is torch.int32 and positions.is_contiguous() and positions.shape == (rope.n_axes, n_tokens)
+    rq, rk = _rope_rows(rope, n_tokens, q, q_out, q_weight), _rope_rows(rope, n_tokens, k, k_out, k_weight)
+    _check(lib().pf_qk_norm_rope(ctypes.byref(rope), n_tokens, _ptr(positions), ctypes.byref(rq), ctypes.byref(rk), float(eps),
+                                 _stream(stream)), "pf_qk_norm_rope")
 
 
 def pf_classify_heads(logits, alpha=0.8, beta=6.4, with_periods=True, stream=None):
