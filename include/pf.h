@@ -362,6 +362,67 @@ typedef struct pf_rope_rows {
 int pf_qk_norm_rope(const pf_rope *rope, int n_tokens, const int32_t *positions, const pf_rope_rows *q,
                     const pf_rope_rows *k, float eps, void *stream);
 
+/* ---- whole prompts, and many sequences behind one prefix ---------------------- */
+
+/*
+ * A batch of packed sequences: sequence s has the query tokens cu_q[s] .. cu_q[s+1]-1 and the key tokens cu_k[s] ..
+ * cu_k[s+1]-1 of its tensors (any of these ranges may be empty; rows behind the last sequence are not touched).
+ * Query heads come in groups of n_heads / n_kv_heads that share a key / value head (head h reads h / group).
+ * The last query of a sequence stands at its last key: query i of lq stands at key place p = lk - lq + i and sees
+ *   block = 0   every key of its sequence;
+ *   block >= 1  the keys j with j / block <= p / block (1: plainly causal; a chunk's tokens: causal by chunks, as a video
+ *               is generated), none if p < 0.
+ * With prefix_tokens > 0 every query also sees that many keys that stand in front of every sequence and are stored once.
+ * cu_q and cu_k are read on the host, during the calls; `work` receives the plan (private format).
+ */
+typedef struct pf_packed {
+  int32_t n_seqs;                 /* >= 1 */
+  int32_t n_heads, n_kv_heads;    /* n_kv_heads divides n_heads */
+  int32_t head_dim;               /* 64 or 128 */
+  int32_t block;                  /* >= 0 */
+  int32_t prefix_tokens;          /* >= 0 */
+  int32_t reserved;               /* must be 0 */
+  /* [lib] written by pf_packed_plan */
+  int32_t n_items, n_planes;      /* work items; partial results that a row may have */
+  int32_t total_q, total_k;       /* tokens planned for */
+  int32_t kernel;
+  const int32_t *cu_q;            /* host [n_seqs+1], cu_q[0] = 0, not decreasing */
+  const int32_t *cu_k;            /* host [n_seqs+1], cu_k[0] = 0, not decreasing */
+  void *work;                     /* dev, >= pf_packed_work_bytes, 32-byte aligned */
+  size_t work_bytes;
+} pf_packed;
+
+/* Bytes of pf_packed.work that pf_packed_plan needs for these lengths; 0 on a bad argument.  Host only. */
+size_t pf_packed_work_bytes(const pf_packed *packed);
+
+/* Plan the batch: what pf_packed_attn_fwd does for these lengths, heads and block, for any number of calls (the layers of a
+ * model).  Writes `work` on the stream (captured into a graph, a replay writes the same plan again).
+ * PF_ERR_CAPACITY if work_bytes is too small. */
+int pf_packed_plan(pf_packed *packed, void *stream);
+
+/* Bytes of workspace that pf_packed_attn_fwd needs under the plan (partial results of rows whose keys are split); 0 on a bad
+ * argument or a batch that has no plan, never 0 otherwise.  Host only. */
+size_t pf_packed_workspace_bytes(const pf_packed *packed);
+
+/*
+ * Attention of the batch:
+ *   out[i, h] = sum_j softmax_j(scale * q[i, h] . k[j, h / group]) v[j, h / group]
+ * over the prefix and the keys that query i sees (see pf_packed); zeros where it sees none.  bf16 in and out, fp32
+ * accumulation, softmax weights rounded to bf16.  Masked scores never count, whatever K holds there; V has to be finite in
+ * every key that a sequence owns.
+ *   q, out              dev [n_heads][total_q][head_dim] or by q_layout and out_layout
+ *   k, v                dev [n_kv_heads][total_k][head_dim] or by kv_layout
+ *   k_prefix, v_prefix  dev [n_kv_heads][prefix_tokens][head_dim] or by prefix_layout; NULL without a prefix
+ *   softmax_scale       0 = 1/sqrt(head_dim)
+ *   workspace           dev, >= pf_packed_workspace_bytes, 16-byte aligned
+ * 16-byte aligned tensors; a NULL layout = packed per head.  Launches that share a workspace must not overlap in time; the
+ * plan is only read.
+ */
+int pf_packed_attn_fwd(const pf_packed *packed, const void *q, const pf_chunk_layout *q_layout, const void *k, const void *v,
+                       const pf_chunk_layout *kv_layout, const void *k_prefix, const void *v_prefix,
+                       const pf_chunk_layout *prefix_layout, void *out, const pf_chunk_layout *out_layout,
+                       float softmax_scale, void *workspace, size_t workspace_bytes, void *stream);
+
 /* ---- before the hot path: which head gets which policy -------------------- */
 
 /*

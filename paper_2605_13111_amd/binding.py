@@ -18,7 +18,8 @@ PF_SYNC_STRIDE = 32            # int32 words between the per-head counters of pf
 EXPORTS = ["pf_index_work_bytes", "pf_attn_workspace_bytes", "pf_selected_count", "pf_retained_count", "pf_plan_segments",
            "pf_pool_reset", "pf_cache_append", "pf_cache_append_strided", "pf_build_index", "pf_ragged_attn_fwd",
            "pf_ragged_attn_fwd_strided", "pf_classify_heads", "pf_status_string", "pf_set_tuning", "pf_index_status_dev", "pf_ragged_attn_fwd_static",
-           "pf_set_block_trace", "pf_rope_init", "pf_qk_norm_rope"]
+           "pf_set_block_trace", "pf_rope_init", "pf_qk_norm_rope", "pf_packed_work_bytes", "pf_packed_plan",
+           "pf_packed_workspace_bytes", "pf_packed_attn_fwd"]
 
 
 class pf_head_policy(ctypes.Structure):
@@ -66,6 +67,12 @@ class pf_rope_rows(ctypes.Structure):
                 ("reserved", ctypes.c_int32), ("x_layout", pf_chunk_layout), ("out_layout", pf_chunk_layout)]
 
 
+class pf_packed(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_seqs", "n_heads", "n_kv_heads", "head_dim", "block", "prefix_tokens", "reserved", "n_items", "n_planes",
+                                              "total_q", "total_k", "kernel")] + \
+               [("cu_q", ctypes.POINTER(ctypes.c_int32)), ("cu_k", ctypes.POINTER(ctypes.c_int32)), ("work", ctypes.c_void_p), ("work_bytes", ctypes.c_size_t)]
+
+
 _lib = None
 
 
@@ -109,6 +116,15 @@ def lib():
         L.pf_rope_init.argtypes = [P(pf_rope), I, I, I, I, P(ctypes.c_int32), ctypes.c_double, P(pf_rope_scaling)]
         L.pf_qk_norm_rope.restype = I
         L.pf_qk_norm_rope.argtypes = [P(pf_rope), I, V, P(pf_rope_rows), P(pf_rope_rows), ctypes.c_float, V]
+        L.pf_packed_work_bytes.restype = ctypes.c_size_t
+        L.pf_packed_work_bytes.argtypes = [P(pf_packed)]
+        L.pf_packed_plan.restype = I
+        L.pf_packed_plan.argtypes = [P(pf_packed), V]
+        L.pf_packed_workspace_bytes.restype = ctypes.c_size_t
+        L.pf_packed_workspace_bytes.argtypes = [P(pf_packed)]
+        L.pf_packed_attn_fwd.restype = I
+        L.pf_packed_attn_fwd.argtypes = [P(pf_packed), V, P(pf_chunk_layout), V, V, P(pf_chunk_layout), V, V, P(pf_chunk_layout), V, P(pf_chunk_layout),
+                                         ctypes.c_float, V, ctypes.c_size_t, V]
         L.pf_set_block_trace.restype = I
         L.pf_set_block_trace.argtypes = [V, ctypes.c_size_t]
         L.pf_set_tuning.restype = I
@@ -386,6 +402,58 @@ def pf_qk_norm_rope(rope, positions, q, q_out, k=None, k_out=None, q_weight=None
     rq, rk = _rope_rows(rope, n_tokens, q, q_out, q_weight), _rope_rows(rope, n_tokens, k, k_out, k_weight)
     _check(lib().pf_qk_norm_rope(ctypes.byref(rope), n_tokens, _ptr(positions), ctypes.byref(rq), ctypes.byref(rk), float(eps),
                                  _stream(stream)), "pf_qk_norm_rope")
+
+
+class Packed:
+    """A batch of packed sequences: its lengths (``cu_q``, ``cu_k``: token offsets, n_seqs + 1 each, on the host), heads and mask, the
+    plan's buffer and the ``pf_packed`` struct.  block: 0 = no mask, 1 = causal, n = causal by blocks of n tokens."""
+
+    def __init__(self, cu_q, cu_k, n_heads, n_kv_heads, head_dim, block=1, prefix_tokens=0, device="cuda:0"):
+        cu_q, cu_k = [int(x) for x in cu_q], [int(x) for x in cu_k]
+        assert len(cu_q) == len(cu_k) and len(cu_q) >= 2
+        n = len(cu_q)
+        self.cu_q, self.cu_k = (ctypes.c_int32 * n)(*cu_q), (ctypes.c_int32 * n)(*cu_k)
+        self.total_q, self.total_k = cu_q[-1], cu_k[-1]
+        self.n_heads, self.n_kv_heads, self.D, self.prefix_tokens, self.device = int(n_heads), int(n_kv_heads), int(head_dim), int(prefix_tokens), torch.device(device)
+        I = ctypes.POINTER(ctypes.c_int32)
+        self.c = pf_packed(n - 1, self.n_heads, self.n_kv_heads, self.D, int(block), self.prefix_tokens, 0, 0, 0, -1, -1, 0,
+                           ctypes.cast(self.cu_q, I), ctypes.cast(self.cu_k, I), 0, 0)
+        nbytes = int(lib().pf_packed_work_bytes(ctypes.byref(self.c)))
+        if nbytes == 0:
+            raise PfError(PF_ERR_UNSUPPORTED if self.D not in (64, 128) else PF_ERR_INVALID_ARG, "pf_packed_work_bytes")
+        self.work = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        self.c.work, self.c.work_bytes = self.work.data_ptr(), nbytes
+
+
+def pf_packed_plan(packed, stream=None):
+    _check(lib().pf_packed_plan(ctypes.byref(packed.c), _stream(stream)), "pf_packed_plan")
+
+
+def pf_packed_workspace_bytes(packed):
+    return int(lib().pf_packed_workspace_bytes(ctypes.byref(packed.c)))
+
+
+def _packed_layout(heads, tokens, D, *tensors):
+    """Checks of tensors that share a layout; the layout.  They may hold more tokens than the batch has."""
+    shape, stride = tensors[0].shape, tensors[0].stride()
+    assert shape[0] == heads and shape[1] >= tokens and shape[2] == D and stride[2] == 1
+    for t in tensors:
+        assert t.dtype is _BF16 and t.shape == shape and t.stride() == stride
+    return pf_chunk_layout(stride[1], stride[0])
+
+
+def pf_packed_attn_fwd(packed, q, k, v, out, workspace, k_prefix=None, v_prefix=None, softmax_scale=0.0, stream=None):
+    """q, out: bf16 views of logical shape [n_heads, total_q, head_dim]; k, v: [n_kv_heads, total_k, head_dim]; k_prefix, v_prefix:
+    [n_kv_heads, prefix_tokens, head_dim] -- e.g. [tokens, heads, head_dim] tensors seen heads first; no copy is made.  k and v share a
+    stride pattern, and so do the prefix's.  workspace: uint8 tensor."""
+    ql, ol = _packed_layout(packed.n_heads, packed.total_q, packed.D, q), _packed_layout(packed.n_heads, packed.total_q, packed.D, out)
+    kl = _packed_layout(packed.n_kv_heads, packed.total_k, packed.D, k, v)
+    pl = None
+    if packed.prefix_tokens:
+        pl = ctypes.byref(_packed_layout(packed.n_kv_heads, packed.prefix_tokens, packed.D, k_prefix, v_prefix))
+    _check(lib().pf_packed_attn_fwd(ctypes.byref(packed.c), q.data_ptr(), ctypes.byref(ql), k.data_ptr(), v.data_ptr(), ctypes.byref(kl), _ptr(k_prefix),
+                                    _ptr(v_prefix), pl, out.data_ptr(), ctypes.byref(ol), float(softmax_scale), _ptr(workspace),
+                                    0 if workspace is None else workspace.nbytes, _stream(stream)), "pf_packed_attn_fwd")
 
 
 def pf_classify_heads(logits, alpha=0.8, beta=6.4, with_periods=True, stream=None):

@@ -1,0 +1,353 @@
+"""Attention of packed sequences, alone and behind a shared prefix (pf_packed_plan, pf_packed_attn_fwd): refusals on the CPU, results on
+the GPU against the definition in 64 bits."""
+import ctypes
+import math
+import os
+
+import pytest
+import torch
+
+from paper_2605_13111_amd import binding as B
+from paper_2605_13111_amd import synth
+
+pytestmark = pytest.mark.skipif(not os.path.exists(B.LIB_PATH), reason="libpf.so not built")
+DEV = "cuda:0"
+
+
+def _cu(lengths):
+    out = [0]
+    for n in lengths:
+        out.append(out[-1] + n)
+    return out
+
+
+# ---- refusals ---------------------------------------------------------------------------------------------------------
+
+def _struct(cu_q=(0, 5, 9), cu_k=(0, 5, 9), heads=4, kv=2, D=128, block=1, prefix=0, reserved=0, work=0x1000, work_bytes=1 << 20, seqs=None):
+    a, b = (ctypes.c_int32 * len(cu_q))(*cu_q), (ctypes.c_int32 * len(cu_k))(*cu_k)
+    I = ctypes.POINTER(ctypes.c_int32)
+    s = B.pf_packed(len(cu_q) - 1 if seqs is None else seqs, heads, kv, D, block, prefix, reserved, 0, 0, -1, -1, 0, ctypes.cast(a, I), ctypes.cast(b, I), work, work_bytes)
+    s._keep = (a, b)
+    return s
+
+
+BAD = [dict(cu_q=(1, 5, 9)), dict(cu_k=(1, 5, 9)), dict(cu_q=(0, 5, 4)), dict(cu_k=(0, 5, 4)), dict(heads=0), dict(kv=0), dict(kv=3), dict(heads=1026, kv=2),
+       dict(block=-1), dict(prefix=-1), dict(prefix=(1 << 24) + 1), dict(reserved=1), dict(seqs=0), dict(seqs=(1 << 20) + 1), dict(cu_q=(0, 1, (1 << 24) + 1)),
+       dict(cu_k=(0, 1, (1 << 30) + 1)), dict(cu_q=(0, 1, 1 << 22), heads=512)]
+
+
+@pytest.mark.parametrize("kw", BAD)
+def test_batches_refused(kw):
+    s, L = _struct(**kw), B.lib()
+    assert L.pf_packed_work_bytes(ctypes.byref(s)) == 0 and L.pf_packed_workspace_bytes(ctypes.byref(s)) == 0
+    assert L.pf_packed_plan(ctypes.byref(s), None) == B.PF_ERR_INVALID_ARG
+    fake = ctypes.c_void_p(0x10000)
+    assert L.pf_packed_attn_fwd(ctypes.byref(s), fake, None, fake, fake, None, None, None, None, fake, None, 0.0, None, 0, None) == B.PF_ERR_INVALID_ARG
+
+
+def test_plans_refused():
+    L = B.lib()
+    assert L.pf_packed_plan(None, None) == B.PF_ERR_INVALID_ARG and L.pf_packed_work_bytes(None) == 0
+    assert L.pf_packed_plan(ctypes.byref(_struct(D=96)), None) == B.PF_ERR_UNSUPPORTED
+    assert L.pf_packed_plan(ctypes.byref(_struct(work=0)), None) == B.PF_ERR_INVALID_ARG
+    assert L.pf_packed_plan(ctypes.byref(_struct(work=0x1008)), None) == B.PF_ERR_INVALID_ARG
+    s = _struct()
+    need = L.pf_packed_work_bytes(ctypes.byref(s))
+    assert need > 0
+    s.work_bytes = need - 1
+    assert L.pf_packed_plan(ctypes.byref(s), None) == B.PF_ERR_CAPACITY
+    with pytest.raises(B.PfError) as e:
+        B.Packed([0, 4], [0, 4], 4, 4, 96, device="cpu")
+    assert e.value.status == B.PF_ERR_UNSUPPORTED
+
+
+def test_calls_refused_without_a_device():
+    """A struct filled in as a plan would (no plan is uploaded: every refusal comes before anything is enqueued)."""
+    L, bad, fake = B.lib(), B.PF_ERR_INVALID_ARG, 0x10000
+
+    def call(s, q=fake, k=fake, v=fake, out=fake, kp=0, vp=0, ql=(512, 128), kl=(256, 128), pl=None, ol=None, scale=0.0, ws=0, ws_bytes=0):
+        lay = lambda x: None if x is None else ctypes.byref(B.pf_chunk_layout(*x))
+        return L.pf_packed_attn_fwd(ctypes.byref(s), q, lay(ql), k, v, lay(kl), kp, vp, lay(pl), out, lay(ql if ol is None else ol), scale, ws, ws_bytes, None)
+
+    def planned(**kw):
+        s = _struct(**kw)
+        s.n_items, s.n_planes, s.total_q, s.total_k = 4, 0, s._keep[0][len(s._keep[0]) - 1], s._keep[1][len(s._keep[1]) - 1]
+        return s
+
+    assert call(_struct()) == bad                                 # never planned
+    empty = planned(cu_q=(0, 0, 0))
+    assert call(empty, q=0, out=0) == B.PF_OK                     # no query, nothing enqueued
+    s = planned()
+    for kw in (dict(q=0), dict(k=0), dict(v=0), dict(out=0), dict(q=fake + 8), dict(k=fake + 2), dict(v=fake + 8), dict(out=fake + 8), dict(ql=(512, 127)),
+               dict(ql=(256, 128)), dict(ol=(512, 120)), dict(ol=(384, 128)), dict(kl=(128, 128)), dict(ws=0x10008), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf"))):
+        assert call(s, **kw) == bad, kw
+    s = planned()
+    s.total_k = 8                                                 # planned for other lengths
+    assert call(s) == bad
+    s = planned(work_bytes=64)                                    # four items do not fit
+    assert call(s) == bad
+    s = planned(work=0)
+    assert call(s) == bad
+    s = planned(prefix=10)
+    s.n_planes = 2
+    need = 2 * 9 * 4 * (128 * 4 + 8)
+    assert L.pf_packed_workspace_bytes(ctypes.byref(s)) >= need
+    assert call(s, ws=0x20000, ws_bytes=need) == bad              # no prefix tensors
+    assert call(s, kp=fake, vp=fake, pl=(256, 128)) == bad        # no workspace
+    assert call(s, kp=fake, vp=fake, pl=(256, 128), ws=0x20000, ws_bytes=need - 1) == bad
+    assert call(s, kp=fake, vp=fake, pl=(128, 128), ws=0x20000, ws_bytes=need) == bad
+
+
+# ---- results ----------------------------------------------------------------------------------------------------------
+
+def _definition(q, k, v, cu_q, cu_k, block, kp=None, vp=None, scale=None):
+    """q [H, tq, D], k / v [KV, tk, D], kp / vp [KV, P, D] -> out [H, tq, D] in 64 bits and the error that the kernel's arithmetic may have:
+      every weight rounded to bf16 (2^-8 of what it multiplies) and the result too (2^-8 of itself);
+      a score off by (D + 4) 2^-24 of the sum of its products' sizes, plus 2^-20 for the exponent's argument and the power, which
+      moves a weight by that factor, numerator and sum alike; n additions of 2^-24 each."""
+    H, tq, D = q.shape
+    G, scale = H // k.shape[0], D ** -0.5 if scale is None else scale
+    out, tol = torch.zeros((H, tq, D), dtype=torch.float64, device=q.device), torch.zeros((H, tq, D), dtype=torch.float64, device=q.device)
+    for s in range(len(cu_q) - 1):
+        q0, q1, k0, k1 = cu_q[s], cu_q[s + 1], cu_k[s], cu_k[s + 1]
+        for h in range(H):
+            K, V, P = k[h // G, k0:k1].double(), v[h // G, k0:k1].double(), 0
+            if kp is not None:
+                P = kp.shape[1]
+                K, V = torch.cat([kp[h // G].double(), K]), torch.cat([vp[h // G].double(), V])
+            if q1 == q0 or K.shape[0] == 0:
+                continue
+            x = q[h, q0:q1].double() @ K.T * scale
+            seen = torch.ones(x.shape, dtype=torch.bool, device=q.device)
+            if block:
+                place = torch.arange(q1 - q0, device=q.device) + (k1 - k0) - (q1 - q0)
+                j = torch.arange(K.shape[0], device=q.device) - P
+                seen = (j[None] < 0) | (torch.div(j[None], block, rounding_mode="floor") <= torch.div(place[:, None], block, rounding_mode="floor"))
+            x = torch.where(seen, x, -math.inf)
+            some = seen.any(1, keepdim=True)
+            w = torch.where(some, torch.softmax(x, 1), 0.0)
+            V0 = torch.where(seen.any(0)[:, None], V, 0.0)
+            out[h, q0:q1] = w @ V0
+            size = torch.where(seen, (q[h, q0:q1].double().abs() @ K.abs().T) * scale, 0.0).amax(1, keepdim=True)
+            d = size * (D + 4) * 2.0 ** -24 + 2.0 ** -20
+            A = w @ V0.abs()
+            tol[h, q0:q1] = 2.0 ** -8 * out[h, q0:q1].abs() + A * (1 + 2.0 ** -8) * (2.0 ** -8 + 2 * d + K.shape[0] * 2.0 ** -24) + 1e-38
+    return out, tol
+
+
+def _tensors(H, KV, D, tq, tk, P, seed, model, spare=0, gain=1.0):
+    def make(h, n, s):
+        n += spare
+        if model:
+            return synth.randn_bf16((n, h, D), s, device=DEV).transpose(0, 1)
+        return synth.randn_bf16((h, n, D), s, device=DEV)
+    q, k, v = make(H, tq, seed) * gain, make(KV, tk, seed + 1), make(KV, tk, seed + 2)
+    spare = 0
+    kp, vp = (make(KV, P, seed + 3), make(KV, P, seed + 4)) if P else (None, None)
+    return q, k, v, kp, vp
+
+
+def _run(cu_q, cu_k, q, k, v, block, kp=None, vp=None, scale=0.0):
+    packed = B.Packed(cu_q, cu_k, q.shape[0], k.shape[0], q.shape[2], block=block, prefix_tokens=0 if kp is None else kp.shape[1], device=DEV)
+    B.pf_packed_plan(packed)
+    # what an earlier use left in the workspace must not matter
+    ws = torch.full((B.pf_packed_workspace_bytes(packed),), 255, dtype=torch.uint8, device=DEV)
+    out = torch.full_like(q, float("nan"))
+    B.pf_packed_attn_fwd(packed, q, k, v, out, ws, kp, vp, softmax_scale=scale)
+    again = torch.full_like(q, float("nan"))
+    B.pf_packed_attn_fwd(packed, q, k, v, again, ws, kp, vp, softmax_scale=scale)
+    torch.cuda.synchronize()
+    n = cu_q[-1]
+    assert torch.equal(out[:, :n].contiguous().view(torch.int16), again[:, :n].contiguous().view(torch.int16))
+    return out
+
+
+def _case(cu_q, cu_k, H, KV, D, block, P, seed=1, model=True, gain=1.0, scale=None, spare=0):
+    q, k, v, kp, vp = _tensors(H, KV, D, cu_q[-1], cu_k[-1], P, seed, model, spare, gain)
+    out = _run(cu_q, cu_k, q, k, v, block, kp, vp, 0.0 if scale is None else scale)
+    want, tol = _definition(q, k, v, cu_q, cu_k, block, kp, vp, scale)
+    n = cu_q[-1]
+    assert torch.isfinite(out[:, :n]).all()
+    over = (out[:, :n].double() - want[:, :n]).abs() - tol[:, :n]
+    assert over.max() <= 0 if over.numel() else True, "off by %.3g more than allowed" % float(over.max())
+    return out, want
+
+
+LENGTHS = {
+    "one": ([1], [1]), "token": ([1], [777]), "tile": ([64], [64]), "odd": ([65, 1, 130], [65, 1, 130]), "empties": ([0, 5, 3, 0, 1], [5, 5, 0, 0, 129]),
+    "long_queries": ([200, 7], [100, 3]), "late": ([3, 129, 33], [400, 257, 1000]), "steps": ([1] * 9, [1, 2, 63, 64, 65, 500, 0, 7, 128]),
+}
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name", sorted(LENGTHS))
+@pytest.mark.parametrize("H,KV,D", [(3, 3, 128), (8, 2, 128), (5, 1, 64), (4, 4, 64)])
+@pytest.mark.parametrize("block,P", [(0, 0), (1, 0), (48, 0), (1, 70), (100, 1), (0, 256)])
+def test_against_the_definition(name, H, KV, D, block, P):
+    lq, lk = LENGTHS[name]
+    _case(_cu(lq), _cu(lk), H, KV, D, block, P, model=(block + P) % 2 == 0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("H,KV,D", [(4, 4, 128), (16, 2, 64), (24, 3, 128)])
+@pytest.mark.parametrize("block,P", [(1, 0), (300, 0), (1, 1500), (0, 0)])
+def test_longer_sequences(H, KV, D, block, P):
+    lq = [1300, 513, 257, 1]
+    _case(_cu(lq), _cu(lq), H, KV, D, block, P, seed=3)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("seqs,P,H,KV", [(1, 0, 8, 1), (1, 9000, 4, 4), (40, 3333, 8, 2), (150, 129, 2, 2)])
+def test_single_tokens_of_many_sequences(D, seqs, P, H, KV):
+    lk = [1 + (i * 37) % 200 for i in range(seqs)] if seqs > 1 else [20000]
+    _case(_cu([1] * seqs), _cu(lk), H, KV, D, 1, P, seed=5)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("gain,scale", [(60.0, None), (1.0, 3.0), (1.0, 1e-4), (30.0, 20.0), (1.0, 1e-30)])
+@pytest.mark.parametrize("D", [64, 128])
+def test_sharp_and_flat_softmax(gain, scale, D):
+    """Scores far apart: the reference maximum moves many times; masked tiles in front of it."""
+    _case(_cu([100, 300]), _cu([100, 300]), 4, 2, D, 1, 90, seed=7, gain=gain, scale=scale)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("P", [0, 100])
+def test_rows_behind_the_last_sequence(D, P):
+    """Tensors longer than the batch: what lies behind may be anything and stays as it is."""
+    cu = _cu([70, 33])
+    q, k, v, kp, vp = _tensors(4, 2, D, 103, 103, P, 11, True, spare=40)
+    kp, vp = (None, None) if P == 0 else (kp[:, :P], vp[:, :P])
+    k[:, 103:], v[:, 103:] = float("nan"), float("inf")
+    out = _run(cu, cu, q, k, v, 1, kp, vp)
+    want, tol = _definition(q[:, :103], k[:, :103], v[:, :103], cu, cu, 1, kp, vp)
+    assert ((out[:, :103].double() - want).abs() <= tol).all() and torch.isnan(out[:, 103:]).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf"), -3.0e38])
+@pytest.mark.parametrize("D", [64, 128])
+def test_masked_keys_do_not_count(bad, D):
+    """K of later tokens may hold anything: the rows that do not see them have the bits that they had."""
+    cu = _cu([200])
+    q, k, v, _, _ = _tensors(4, 4, D, 200, 200, 0, 13, False)
+    out = _run(cu, cu, q, k, v, 1)
+    k[:, 77:] = bad
+    got = _run(cu, cu, q, k, v, 1)
+    assert torch.equal(got[:, :77], out[:, :77])
+
+
+@pytest.mark.gpu
+def test_gaps_between_rows_and_heads():
+    """q, k and v as slices of one projection, the results as a slice of a wider buffer."""
+    H, KV, D, n = 6, 3, 128, 150
+    cu = _cu([100, 50])
+    wide = synth.randn_bf16((n, H + 2 * KV + 1, D), 21, device=DEV)
+    q, k, v = (wide[:, a:b].transpose(0, 1) for a, b in ((0, H), (H, H + KV), (H + KV, H + 2 * KV)))
+    buf = torch.zeros((n, H + 2 * KV + 1, D), dtype=torch.bfloat16, device=DEV)
+    packed = B.Packed(cu, cu, H, KV, D, block=1, device=DEV)
+    B.pf_packed_plan(packed)
+    ws = torch.empty(B.pf_packed_workspace_bytes(packed), dtype=torch.uint8, device=DEV)
+    B.pf_packed_attn_fwd(packed, q, k, v, buf[:, :H].transpose(0, 1), ws)
+    torch.cuda.synchronize()
+    want, tol = _definition(q, k, v, cu, cu, 1)
+    assert ((buf[:, :H].transpose(0, 1).double() - want).abs() <= tol).all() and (buf[:, H:] == 0).all()
+
+
+@pytest.mark.gpu
+def test_offsets_beyond_32_bits():
+    """Keys of 64 heads by 300 000 tokens: 2.4e9 elements a tensor; the last sequence lies beyond 2^32 bytes."""
+    KV, D, tk = 64, 128, 300000
+    g = torch.Generator(device=DEV)
+    g.manual_seed(3)
+    k = torch.empty((tk, KV, D), dtype=torch.bfloat16, device=DEV)
+    v = torch.empty_like(k)
+    for t in (k, v):
+        for i in range(0, tk, 50000):
+            t[i:i + 50000] = torch.randn((50000, KV, D), generator=g, device=DEV).to(torch.bfloat16)
+    k, v = k.transpose(0, 1), v.transpose(0, 1)
+    cu_q, cu_k = _cu([1, 2, 40]), _cu([1000, 298000, 1000])
+    q = synth.randn_bf16((43, KV, D), 5, device=DEV).transpose(0, 1)
+    out = _run(cu_q, cu_k, q, k, v, 1)
+    want, tol = _definition(q, k, v, cu_q, cu_k, 1)
+    assert ((out.double() - want).abs() <= tol).all()
+
+
+@pytest.mark.gpu
+def test_streams_graphs_and_two_batches_at_once():
+    H, KV, D = 8, 2, 128
+    cu_a, cu_b = _cu([300, 41]), _cu([1] * 12)
+    cu_bk = _cu([50 + i for i in range(12)])
+    qa, ka, va, _, _ = _tensors(H, KV, D, cu_a[-1], cu_a[-1], 0, 31, True)
+    qb, kb, vb, kp, vp = _tensors(H, KV, D, cu_b[-1], cu_bk[-1], 700, 41, True)
+    want_a, want_b = _run(cu_a, cu_a, qa, ka, va, 1), _run(cu_b, cu_bk, qb, kb, vb, 1, kp, vp)
+    pa, pb = B.Packed(cu_a, cu_a, H, KV, D, block=1, device=DEV), B.Packed(cu_b, cu_bk, H, KV, D, block=1, prefix_tokens=700, device=DEV)
+    oa, ob = torch.empty_like(qa), torch.empty_like(qb)
+    B.pf_packed_plan(pa)
+    B.pf_packed_plan(pb)
+    wa, wb = (torch.empty(B.pf_packed_workspace_bytes(p), dtype=torch.uint8, device=DEV) for p in (pa, pb))
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    for s in (s1, s2):
+        s.wait_stream(torch.cuda.current_stream())
+    for _ in range(3):                                            # side by side, each with a workspace of its own
+        with torch.cuda.stream(s1):
+            B.pf_packed_attn_fwd(pa, qa, ka, va, oa, wa)
+        with torch.cuda.stream(s2):
+            B.pf_packed_attn_fwd(pb, qb, kb, vb, ob, wb, kp, vp)
+    torch.cuda.synchronize()
+    assert torch.equal(oa, want_a) and torch.equal(ob, want_b)
+    # plan and attention captured, replayed with other inputs, eager work between
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        B.pf_packed_plan(pb)
+        B.pf_packed_attn_fwd(pb, qb, kb, vb, ob, wb, kp, vp)
+    for seed in (51, 52, 53):
+        qb.copy_(synth.randn_bf16((12, H, D), seed, device=DEV).transpose(0, 1))
+        pb.work.zero_()
+        graph.replay()
+        got = ob.clone()
+        want = _run(cu_b, cu_bk, qb, kb, vb, 1, kp, vp)
+        assert torch.equal(got, want)
+
+
+@pytest.mark.gpu
+def test_a_prompt_taken_in_and_continued():
+    """As they are used together: queries and keys of a whole prompt normalised and rotated, the prompt's attention causal by chunks, its
+    keys and values taken into the ragged cache, the next chunk attended to through the cache -- and the same chunk attended to
+    behind the prompt as a shared prefix, twice over."""
+    H, D, tpf, chunk, frames = 3, 128, 40, 2, 6
+    n, Lq = frames * tpf, chunk * tpf
+    rope = B.make_rope(D, axis_pairs=[24, 20, 20], interleaved=True)
+    raw = synth.randn_bf16((n + Lq, 3 * H, D), 61, device=DEV)
+    t = torch.arange(n + Lq, device=DEV, dtype=torch.int32)
+    pos = torch.stack([t // tpf, t % tpf // 8, t % 8]).contiguous()
+    q, k, v = (raw[:, i * H:(i + 1) * H].transpose(0, 1) for i in range(3))
+    B.pf_qk_norm_rope(rope, pos, q, q, k, k, eps=1e-6)
+    # the prompt, and the prompt with the next chunk: the chunk is the last block
+    cu = _cu([n + Lq])
+    whole = _run(cu, cu, q, k, v, Lq)
+    cu = _cu([n])
+    prompt = _run(cu, cu, q[:, :n], k[:, :n], v[:, :n], Lq)
+    assert torch.equal(prompt.contiguous(), whole[:, :n].contiguous())
+    pool = B.Pool([synth.anchor_all(frames)] * H, tpf, D, device=DEV)
+    B.pf_pool_reset(pool)
+    B.pf_cache_append_strided(pool, k[:, :n].unflatten(1, (frames, tpf)), v[:, :n].unflatten(1, (frames, tpf)))
+    index = B.Index(pool, Lq)
+    B.pf_build_index(pool, index, Lq)
+    out = torch.empty((Lq, H, D), dtype=torch.bfloat16, device=DEV).transpose(0, 1)
+    ws = torch.empty(B.pf_attn_workspace_bytes(pool, Lq), dtype=torch.uint8, device=DEV)
+    new = [x[:, n:].contiguous() for x in (q, k, v)]
+    packed_out = torch.empty_like(new[0])
+    B.pf_ragged_attn_fwd(pool, index, *new, packed_out, ws)
+    torch.cuda.synchronize()
+    want, tol = _definition(q, k, v, _cu([n + Lq]), _cu([n + Lq]), Lq)
+    want, tol = want[:, n:], tol[:, n:]
+    for got in (whole[:, n:], packed_out):
+        assert ((got.double() - want).abs() <= tol).all()
+    twice = [torch.cat([x, x], 1) for x in new]
+    cu = _cu([Lq, Lq])
+    both = _run(cu, cu, *twice, Lq, k[:, :n], v[:, :n])
+    for got in (both[:, :Lq], both[:, Lq:]):
+        assert ((got.double() - want).abs() <= tol).all()
