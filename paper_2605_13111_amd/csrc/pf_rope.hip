@@ -18,6 +18,7 @@ typedef __attribute__((ext_vector_type(4))) float rope_f4;
 
 constexpr int ROPE_THREADS = 256;
 constexpr int ROPE_WAVES = ROPE_THREADS / 64;
+constexpr int ROPE_MIN_WAVES = 8192;                              // 32 per compute unit
 constexpr int ROPE_AHEAD = 3;                                     // groups of rows in flight per wave
 
 struct RopeParams {
@@ -253,9 +254,12 @@ extern "C" int pf_qk_norm_rope(const pf_rope *rope, int n_tokens, const int32_t 
   P.n_tokens = n_tokens;
   P.n_q = q->n_heads;
   P.n_rows = q->n_heads + k->n_heads;
-  const int rows = 64 * 8 / D;                                    // that a wave holds side by side
-  P.n_parts = 1;
-  P.rows_per_wave = P.n_rows;
+  // A wave takes a whole token's rows where tokens are many (its cosines and sines then serve all of them), and where waves would be
+  // too few to hide each other's memory latency, as few rows as it holds side by side
+  const int side = 64 * 8 / D, groups = pf_ceil_div(P.n_rows, side);
+  const int parts = (int)(ROPE_MIN_WAVES / n_tokens < groups ? ROPE_MIN_WAVES / n_tokens : groups);
+  P.rows_per_wave = pf_ceil_div(groups, parts < 1 ? 1 : parts) * side;
+  P.n_parts = pf_ceil_div(P.n_rows, P.rows_per_wave);
   P.rot = rope->rot_dim;
   P.pairs_end0 = rope->axis_pairs[0];
   P.pairs_end1 = rope->n_axes > 1 ? rope->axis_pairs[0] + rope->axis_pairs[1] : PF_ROPE_MAX_PAIRS;
@@ -264,7 +268,6 @@ extern "C" int pf_qk_norm_rope(const pf_rope *rope, int n_tokens, const int32_t 
   P.eps = eps;
   P.magnitude = rope->magnitude;
   for (int i = 0; i < PF_ROPE_MAX_PAIRS; ++i) P.turns[i] = i < pairs ? rope->turns[i] : 0.0;
-  (void)rows;
   const long long jobs = (long long)n_tokens * P.n_parts;
   const dim3 grid((unsigned)((jobs + ROPE_WAVES - 1) / ROPE_WAVES));
   hipStream_t st = (hipStream_t)stream;
