@@ -6,6 +6,7 @@ functions raises.
 """
 import ctypes
 import os
+import struct
 
 import torch
 
@@ -115,7 +116,7 @@ def lib():
         L.pf_rope_init.restype = I
         L.pf_rope_init.argtypes = [P(pf_rope), I, I, I, I, P(ctypes.c_int32), ctypes.c_double, P(pf_rope_scaling)]
         L.pf_qk_norm_rope.restype = I
-        L.pf_qk_norm_rope.argtypes = [P(pf_rope), I, V, P(pf_rope_rows), P(pf_rope_rows), ctypes.c_float, V]
+        L.pf_qk_norm_rope.argtypes = [P(pf_rope), I, V, V, V, ctypes.c_float, V]
         L.pf_packed_work_bytes.restype = ctypes.c_size_t
         L.pf_packed_work_bytes.argtypes = [P(pf_packed)]
         L.pf_packed_plan.restype = I
@@ -123,8 +124,7 @@ def lib():
         L.pf_packed_workspace_bytes.restype = ctypes.c_size_t
         L.pf_packed_workspace_bytes.argtypes = [P(pf_packed)]
         L.pf_packed_attn_fwd.restype = I
-        L.pf_packed_attn_fwd.argtypes = [P(pf_packed), V, P(pf_chunk_layout), V, V, P(pf_chunk_layout), V, V, P(pf_chunk_layout), V, P(pf_chunk_layout),
-                                         ctypes.c_float, V, ctypes.c_size_t, V]
+        L.pf_packed_attn_fwd.argtypes = [P(pf_packed), V, V, V, V, V, V, V, V, V, V, ctypes.c_float, V, ctypes.c_size_t, V]
         L.pf_set_block_trace.restype = I
         L.pf_set_block_trace.argtypes = [V, ctypes.c_size_t]
         L.pf_set_tuning.restype = I
@@ -379,17 +379,26 @@ def make_rope(head_dim, rot_dim=None, interleaved=False, axis_pairs=None, base=1
     return rope
 
 
-def _rope_rows(rope, n_tokens, x, out, weight):
+# pf_rope_rows and pf_chunk_layout as bytes: packing them takes a third of what filling ctypes structs takes, and small calls are bound by it
+_ROWS, _LAYOUT = struct.Struct("PPPiiqqqq"), struct.Struct("qq")
+_NO_ROWS = bytes(_ROWS.size)
+assert _ROWS.size == ctypes.sizeof(pf_rope_rows) and _LAYOUT.size == ctypes.sizeof(pf_chunk_layout)
+
+
+def _rope_rows(D, n_tokens, x, out, weight):
     """A tensor and its result as a ``pf_rope_rows`` struct: bf16 views of logical shape [heads, tokens, head_dim]."""
     if x is None:
         assert out is None and weight is None
-        return pf_rope_rows()
-    shape, xs, os_ = x.shape, x.stride(), out.stride()
-    assert x.dtype is _BF16 and out.dtype is _BF16 and out.shape == shape and shape[1:] == (n_tokens, rope.head_dim)
-    assert xs[2] == 1 and os_[2] == 1
-    if weight is not None:
-        assert weight.dtype is _BF16 and weight.shape == (rope.head_dim,) and weight.is_contiguous()
-    return pf_rope_rows(x.data_ptr(), out.data_ptr(), _ptr(weight), shape[0], 0, pf_chunk_layout(xs[1], xs[0]), pf_chunk_layout(os_[1], os_[0]))
+        return _NO_ROWS
+    shape = x.shape
+    heads, tokens, d = shape
+    xh, xt, x1 = x.stride()
+    oh, ot, o1 = out.stride()
+    assert x.dtype is _BF16 and out.dtype is _BF16 and out.shape == shape and tokens == n_tokens and d == D and x1 == 1 and o1 == 1
+    if weight is None:
+        return _ROWS.pack(x.data_ptr(), out.data_ptr(), 0, heads, 0, xt, xh, ot, oh)
+    assert weight.dtype is _BF16 and weight.shape == (D,) and weight.is_contiguous()
+    return _ROWS.pack(x.data_ptr(), out.data_ptr(), weight.data_ptr(), heads, 0, xt, xh, ot, oh)
 
 
 def pf_qk_norm_rope(rope, positions, q, q_out, k=None, k_out=None, q_weight=None, k_weight=None, eps=0.0, stream=None):
@@ -399,9 +408,9 @@ def pf_qk_norm_rope(rope, positions, q, q_out, k=None, k_out=None, q_weight=None
     n_tokens = (k if q is None else q).shape[1]
     if rope.rot_dim:
         assert positions.dtype is torch.int32 and positions.is_contiguous() and positions.shape == (rope.n_axes, n_tokens)
-    rq, rk = _rope_rows(rope, n_tokens, q, q_out, q_weight), _rope_rows(rope, n_tokens, k, k_out, k_weight)
-    _check(lib().pf_qk_norm_rope(ctypes.byref(rope), n_tokens, _ptr(positions), ctypes.byref(rq), ctypes.byref(rk), float(eps),
-                                 _stream(stream)), "pf_qk_norm_rope")
+    D = rope.head_dim
+    _check(lib().pf_qk_norm_rope(ctypes.byref(rope), n_tokens, _ptr(positions), _rope_rows(D, n_tokens, q, q_out, q_weight),
+                                 _rope_rows(D, n_tokens, k, k_out, k_weight), eps, _stream(stream)), "pf_qk_norm_rope")
 
 
 class Packed:
@@ -433,27 +442,27 @@ def pf_packed_workspace_bytes(packed):
     return int(lib().pf_packed_workspace_bytes(ctypes.byref(packed.c)))
 
 
-def _packed_layout(heads, tokens, D, *tensors):
-    """Checks of tensors that share a layout; the layout.  They may hold more tokens than the batch has."""
-    shape, stride = tensors[0].shape, tensors[0].stride()
-    assert shape[0] == heads and shape[1] >= tokens and shape[2] == D and stride[2] == 1
-    for t in tensors:
-        assert t.dtype is _BF16 and t.shape == shape and t.stride() == stride
-    return pf_chunk_layout(stride[1], stride[0])
+def _packed_layout(heads, tokens, D, a, b=None):
+    """Checks of a tensor, or of two that share a layout; the layout.  They may hold more tokens than the batch has."""
+    shape, stride = a.shape, a.stride()
+    assert shape[0] == heads and shape[1] >= tokens and shape[2] == D and stride[2] == 1 and a.dtype is _BF16
+    assert b is None or (b.dtype is _BF16 and b.shape == shape and b.stride() == stride)
+    return _LAYOUT.pack(stride[1], stride[0])
 
 
 def pf_packed_attn_fwd(packed, q, k, v, out, workspace, k_prefix=None, v_prefix=None, softmax_scale=0.0, stream=None):
     """q, out: bf16 views of logical shape [n_heads, total_q, head_dim]; k, v: [n_kv_heads, total_k, head_dim]; k_prefix, v_prefix:
     [n_kv_heads, prefix_tokens, head_dim] -- e.g. [tokens, heads, head_dim] tensors seen heads first; no copy is made.  k and v share a
     stride pattern, and so do the prefix's.  workspace: uint8 tensor."""
-    ql, ol = _packed_layout(packed.n_heads, packed.total_q, packed.D, q), _packed_layout(packed.n_heads, packed.total_q, packed.D, out)
-    kl = _packed_layout(packed.n_kv_heads, packed.total_k, packed.D, k, v)
-    pl = None
+    H, KV, tq, D = packed.n_heads, packed.n_kv_heads, packed.total_q, packed.D
+    kp = vp = pl = None
     if packed.prefix_tokens:
-        pl = ctypes.byref(_packed_layout(packed.n_kv_heads, packed.prefix_tokens, packed.D, k_prefix, v_prefix))
-    _check(lib().pf_packed_attn_fwd(ctypes.byref(packed.c), q.data_ptr(), ctypes.byref(ql), k.data_ptr(), v.data_ptr(), ctypes.byref(kl), _ptr(k_prefix),
-                                    _ptr(v_prefix), pl, out.data_ptr(), ctypes.byref(ol), float(softmax_scale), _ptr(workspace),
-                                    0 if workspace is None else workspace.nbytes, _stream(stream)), "pf_packed_attn_fwd")
+        pl = _packed_layout(KV, packed.prefix_tokens, D, k_prefix, v_prefix)
+        kp, vp = k_prefix.data_ptr(), v_prefix.data_ptr()
+    _check(lib().pf_packed_attn_fwd(ctypes.byref(packed.c), q.data_ptr(), _packed_layout(H, tq, D, q), k.data_ptr(), v.data_ptr(),
+                                    _packed_layout(KV, packed.total_k, D, k, v), kp, vp, pl, out.data_ptr(), _packed_layout(H, tq, D, out),
+                                    softmax_scale, _ptr(workspace), 0 if workspace is None else workspace.nbytes, _stream(stream)),
+           "pf_packed_attn_fwd")
 
 
 def pf_classify_heads(logits, alpha=0.8, beta=6.4, with_periods=True, stream=None):

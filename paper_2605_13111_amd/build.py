@@ -80,9 +80,10 @@ def build(verbose=False, extra=()):
             print(" ".join(cmd), flush=True)
         procs.append((src, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
         objs.append(obj)
-    # device listing of the attention kernels, for the register check above (compiled next to the objects)
-    lst = subprocess.Popen([HIPCC] + FLAGS + list(extra) + ["--cuda-device-only", "-S", os.path.join(CSRC, "pf_attn.hip"), "-o", "-"],
-                           stdout=subprocess.PIPE, stderr=subprocess.DEVNULL, text=True)
+    # device listings of the attention kernels, for the checks above (compiled next to the objects)
+    listing_of = lambda src: subprocess.Popen([HIPCC] + FLAGS + list(extra) + ["--cuda-device-only", "-S", os.path.join(CSRC, src), "-o", "-"],
+                                              stdout=subprocess.PIPE, stderr=subprocess.DEVNULL, text=True)
+    lst, lst_packed = listing_of("pf_attn.hip"), listing_of("pf_packed.hip")
     failed = False
     for src, p in procs:
         out, _ = p.communicate()
@@ -92,10 +93,12 @@ def build(verbose=False, extra=()):
         if lines and (verbose or p.returncode != 0):
             print("\n".join(lines), file=sys.stderr)
     listing, _ = lst.communicate()
-    if failed or lst.returncode != 0:
+    packed_listing, _ = lst_packed.communicate()
+    if failed or lst.returncode != 0 or lst_packed.returncode != 0:
         raise RuntimeError("hipcc failed")
     highest = check_hidden_registers(listing)
     check_scalar_operands(listing)
+    check_scalar_operands(packed_listing)
     if verbose:
         print("64-row attention kernel: highest accumulation register used by the compiler: a%d" % highest, flush=True)
     subprocess.check_call([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB] + objs)

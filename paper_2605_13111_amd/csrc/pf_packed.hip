@@ -6,10 +6,12 @@
 // stands at the last key); a query that sees no key gets zeros.
 //
 // The rows of a key head are the queries of its group: row r of a sequence is query r / group of head kv_head * group + r % group, so that
-// a group reads its keys and values once.  In front of the prefix all sequences' queries make one long line of rows.  A work item is a tile of
-// rows against a run of key tiles: the host cuts the work into items and orders them (pf_packed_plan), heaviest first.  A row tile whose
-// keys are cut into several items, or that has a prefix in front, parks unnormalised partial results (O, m, l) in fp32, one plane per
-// item, row by row; a second kernel joins them in a fixed order.  A launch boundary stands between: no counters, no waiting.
+// a group reads its keys and values once.  A line of rows is one sequence's; its keys are the prefix's tiles and then its own.  Sequences
+// of few rows (single tokens) would each read the prefix for a tile of which they fill little: in front of the prefix they are stacked,
+// neighbours in one line, and each has its own keys as another line.  A work item is a tile of rows against a run of key tiles of its
+// line: the host cuts the work into items and orders them (pf_packed_plan), heaviest first.  Rows whose keys are cut into several items
+// park unnormalised partial results (O, m, l) in fp32, one plane per item, row by row; a second kernel joins them in a fixed order.  A
+// launch boundary stands between: no counters, no waiting.
 //
 // Scores, softmax and value products as in the ragged-cache kernels: S^T = K Q^T and O^T += V^T P^T on 32x32x16 bf16 MFMAs with fp32
 // accumulation, one query row per lane; weights are rounded to bf16 for the second product (2^-8 relative at most each, the sum is
@@ -17,7 +19,9 @@
 #include <math.h>
 #include <string.h>
 #include <algorithm>
+#include <functional>
 #include <new>
+#include <queue>
 #include <vector>
 #include "pf_packed_steps.h"
 
@@ -28,15 +32,18 @@ struct __attribute__((aligned(32))) PackedItem {
   int32_t row0;        // first row of the tile in that line
   int32_t n_rows;      // rows of the whole line
   int32_t k_base;      // token of the line's first key
-  int32_t n_keys;      // keys of the line
-  int32_t kt0, kt1;    // key tiles of this item
-  int32_t head;        // key head | prefix flag << 12 | (plane + 1) << 13 (0: unsplit) | further planes without an item << 22
+  int32_t n_keys;      // keys of the line behind the prefix
+  int32_t kt0, kt1;    // key tiles of this item: the prefix's (if the line has it), then the line's own
+  int32_t head;        // key head | the line has the prefix << 12 | (plane + 1) << 13 (0: unsplit) | further planes without an item << 22 | thin << 31
 };
 constexpr int PACKED_MAX_PLANES = 256;
+constexpr int PACKED_JOIN_BATCHES = PACKED_MAX_PLANES / 64;
+constexpr int PACKED_FEW_PLANES = 4;
 constexpr int PACKED_PREFIX_BIT = 12;
 PF_HD int packed_head(const PackedItem &it) { return it.head & 0xfff; }
-PF_HD bool packed_is_prefix(const PackedItem &it) { return (it.head >> PACKED_PREFIX_BIT) & 1; }
+PF_HD bool packed_has_prefix(const PackedItem &it) { return (it.head >> PACKED_PREFIX_BIT) & 1; }
 PF_HD int packed_plane(const PackedItem &it) { return ((it.head >> 13) & 0x1ff) - 1; }
+PF_HD bool packed_is_thin(const PackedItem &it) { return it.head < 0; }
 PF_HD int packed_missing(const PackedItem &it) { return (it.head >> 22) & 0x1ff; }
 
 // Items reach the device as kernel arguments: the call neither allocates nor waits, and can be captured.
@@ -49,7 +56,9 @@ __global__ void pf_packed_upload_kernel(PackedUpload U, int n, PackedItem *to) {
   if (i < n) to[i] = U.item[i];
 }
 
-constexpr int PACKED_ROWS = 128;                                  // rows of an item: 4 waves x 32
+constexpr int PACKED_WAVES = 4;
+constexpr int PACKED_ROWS = 32 * PACKED_WAVES;                    // rows of a full item
+constexpr int PACKED_THIN_ROWS = 32;                              // lines of at most so many rows are thin items
 
 struct PackedParams {
   const __bf16 *q, *k, *v, *k_prefix, *v_prefix;
@@ -59,9 +68,35 @@ struct PackedParams {
   float2 *part_ml;                                                // [planes][rows]: reference maximum, sum of weights; a sum of -1 in plane 0: the row is done
   long long q_tok, q_head, out_tok, out_head, kv_tok, kv_head, pre_tok, pre_head;    // element strides
   int n_rows, n_heads, group, block;                              // n_rows: tokens x heads
-  int planes;
+  int planes, prefix_tokens, prefix_tiles;
+  unsigned group_mul, group_shift;                                // n / group = (n * group_mul) >> 32 >> group_shift
   float scale_log2;
 };
+
+template <class T>
+__device__ __forceinline__ T *packed_global(T *p) {
+  return (T *)(__attribute__((address_space(1))) T *)(unsigned long long)p;
+}
+// The parameters, read again from the kernel-argument segment at every call (a few scalar loads): held in registers through the loop over the
+// key tiles they would crowd out its own scalars, which the copies need as such.
+__device__ __forceinline__ PackedParams packed_params() {
+  static_assert(sizeof(PackedParams) % 8 == 0, "parameters are copied as 8-byte words");
+  struct Words {
+    unsigned long long w[sizeof(PackedParams) / 8];
+  };
+  int zero = 0;                                                   // hides from the compiler that every call reads the same words
+  asm volatile("" : "+s"(zero));
+  const __attribute__((address_space(4))) unsigned long long *arg =
+      (const __attribute__((address_space(4))) unsigned long long *)__builtin_amdgcn_kernarg_segment_ptr() + __builtin_amdgcn_readfirstlane(zero);
+  Words words;
+#pragma unroll
+  for (int i = 0; i < (int)(sizeof(PackedParams) / 8); ++i) words.w[i] = arg[i];
+  PackedParams P = __builtin_bit_cast(PackedParams, words);
+  P.q = packed_global(P.q), P.k = packed_global(P.k), P.v = packed_global(P.v), P.k_prefix = packed_global(P.k_prefix);
+  P.v_prefix = packed_global(P.v_prefix), P.out = packed_global(P.out), P.items = packed_global(P.items);
+  P.part_o = packed_global(P.part_o), P.part_ml = packed_global(P.part_ml);
+  return P;
+}
 
 template <int D>
 struct PackedTile {
@@ -77,245 +112,557 @@ struct PackedTile {
   static __device__ constexpr int swz_v(int r) { return D == 128 ? (r & 3) << 2 : ((r >> 1) & 1) << 2; }
 };
 
-// keys that row r of the item's line may see
+// n / group by multiplication (n < 2^31; see packed_group): divisions by a number known at run time are some 25 instructions each, and there
+// are several for every row of a tile
+__device__ __forceinline__ int packed_div_group(const PackedParams &P, int n) {
+  return P.group == 1 ? n : (int)(__umulhi((unsigned)n, P.group_mul) >> P.group_shift);
+}
+
+// keys behind the prefix that row r of the item's line may see
 __device__ __forceinline__ int packed_limit(const PackedParams &P, const PackedItem &it, int r) {
-  if (packed_is_prefix(it) || P.block == 0) return it.n_keys;
-  const int place = it.n_keys - it.n_rows / P.group + r / P.group;
+  if (P.block == 0) return it.n_keys;
+  const int place = it.n_keys - packed_div_group(P, it.n_rows) + packed_div_group(P, r);
   if (place < 0) return 0;
+  if (P.block == 1) return place + 1;
   // the last key of the row's block; the block's number and its end stay below 2^31 for any block size (a sequence has at most 2^30 keys)
   const unsigned number = (unsigned)place / (unsigned)P.block;
   return (int)min((unsigned)it.n_keys, number * (unsigned)P.block + (unsigned)P.block);
 }
 
-template <int D>
-__global__ __launch_bounds__(256, D == 128 ? 2 : 4) void pf_packed_attn_kernel(PackedParams P) {
+// Where the keys of an item's tiles sit: one key head of the prefix, and of the line's own keys behind it.
+struct PackedKeys {
+  const __bf16 *k, *v, *k_pre, *v_pre;
+  int pre;             // tiles of the prefix
+};
+__device__ __forceinline__ PackedKeys packed_keys(const PackedParams &P, const PackedItem &it) {
+  PackedKeys K;
+  const int h = packed_head(it);
+  const long long own = (long long)it.k_base * P.kv_tok + h * P.kv_head;
+  K.pre = packed_has_prefix(it) ? P.prefix_tiles : 0;
+  K.k = P.k + own;
+  K.v = P.v + own;
+  K.k_pre = P.k_prefix + h * P.pre_head;
+  K.v_pre = P.v_prefix + h * P.pre_head;
+  return K;
+}
+// Send the copies of ROWS rows of key tile kt, from row r0 on, of K (V) into `to` (a place whose row number in its tile is a multiple of 16).
+template <int D, bool IS_V, int ROWS>
+__device__ __forceinline__ void packed_copy(const PackedParams &P, const PackedItem &it, const PackedKeys &K, int kt, int r0, char *to, int lane) {
   typedef PackedTile<D> C;
   typedef __attribute__((address_space(3))) void *lptr_t;
-  constexpr int WAVES = 4, WROWS = PF_BK / WAVES;                 // tile rows that one wave copies
-  constexpr int NC = WROWS / C::COPY_ROWS;
-  constexpr int SMEM = 2 * C::STAGE_BYTES > PACKED_ROWS * C::LD * 4 ? 2 * C::STAGE_BYTES : PACKED_ROWS * C::LD * 4;
-  __shared__ __attribute__((aligned(1024))) char smem[SMEM];
-  __shared__ float2 s_ml[PACKED_ROWS];
-  const PackedItem it = P.items[blockIdx.x];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int l32 = lane & 31, g = lane >> 5;
-  const bool prefix = packed_is_prefix(it);
-  const int kvh = packed_head(it);
-  const float c = P.scale_log2;
-  const long long tok = prefix ? P.pre_tok : P.kv_tok;
-  const long long k0 = (long long)(it.k_base + it.kt0 * PF_BK) * tok + kvh * (prefix ? P.pre_head : P.kv_head);
-  const __bf16 *kb = (prefix ? P.k_prefix : P.k) + k0, *vb = (prefix ? P.v_prefix : P.v) + k0;
-  const int key0 = it.kt0 * PF_BK, n_tiles = it.kt1 - it.kt0;
+  const bool in_prefix = kt < K.pre;
+  const long long tok = in_prefix ? P.pre_tok : P.kv_tok;
+  const int key0 = (in_prefix ? kt : kt - K.pre) * PF_BK + r0;
+  const __bf16 *b = (in_prefix ? (IS_V ? K.v_pre : K.k_pre) : (IS_V ? K.v : K.k)) + key0 * tok;
   const unsigned rb = (unsigned)(tok * 2);                        // bytes between key rows (below 2^25: checked on the host)
+  const int last = (in_prefix ? P.prefix_tokens : it.n_keys) - 1 - key0;
+  const int rr = lane / C::CHUNKS, p = lane % C::CHUNKS;
+  const unsigned low = (unsigned)((p ^ (IS_V ? C::swz_v(rr) : C::swz_k(rr))) << 4);
+  const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void *)b, 0, -1, 0x00020000u);
+  if (__builtin_expect(last >= ROWS - 1, 1)) {
+    const unsigned at = (unsigned)rr * rb;
+    static_for<0, ROWS / C::COPY_ROWS>([&](auto gi) {
+      constexpr int G = decltype(gi)::value;
+      constexpr unsigned flip = (unsigned)((IS_V ? C::swz_v(G * C::COPY_ROWS) : C::swz_k(G * C::COPY_ROWS)) << 4);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lptr_t)(to + G * 1024), 16, at + (low ^ flip), G * C::COPY_ROWS * rb, 0, 0);
+    });
+  } else {                                                        // rows past the end repeat the last key (or, past a whole step, the one before)
+    int lane_l = lane;
+    asm volatile("" : "+v"(lane_l));                              // rare: its lane offsets are not held in registers through the loop
+    const unsigned low_l = (unsigned)((lane_l % C::CHUNKS ^ (IS_V ? C::swz_v(lane_l / C::CHUNKS) : C::swz_k(lane_l / C::CHUNKS))) << 4);
+    const __amdgpu_buffer_rsrc_t e = __builtin_amdgcn_make_buffer_rsrc((void *)(b + (long long)pf_min(last, 0) * tok), 0, -1, 0x00020000u);
+    static_for<0, ROWS / C::COPY_ROWS>([&](auto gi) {
+      constexpr int G = decltype(gi)::value;
+      constexpr unsigned flip = (unsigned)((IS_V ? C::swz_v(G * C::COPY_ROWS) : C::swz_k(G * C::COPY_ROWS)) << 4);
+      const unsigned at = (unsigned)pf_min(G * C::COPY_ROWS + lane_l / C::CHUNKS, pf_max(last, 0)) * rb;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(e, (lptr_t)(to + G * 1024), 16, at + (low_l ^ flip), 0, 0, 0);
+    });
+  }
+}
 
-  // this lane's query row
+// One row's softmax state.  The reference maximum starts below every score; its multiple is kept finite, so that a masked key's weight against
+// it is 0 and not NaN.
+struct PackedRow {
+  float m, l, mc;
+};
+__device__ __forceinline__ float packed_mc(float m, float c) { return fmaxf(m * c, -3.0e38f); }
+
+// Scores of NKB blocks of 32 keys (accumulators of K Q^T: register i of block kb is key 32 kb + 8 (i / 4) + 4 g + i % 4) -> weights in bf16,
+// the row's state and O moved on.
+template <int D, int NKB>
+__device__ __forceinline__ void packed_softmax(f32x16 (&s)[NKB], bf16x8 (&pf)[2 * NKB], f32x16 (&o)[D / 32], PackedRow &R, float c) {
+  float ts[2];
+  auto weights = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int kb = 0; kb < NKB; ++kb)
+#pragma unroll
+      for (int i = 0; i < 16; i += 2) {
+        const float e0 = fast_exp2(fmaf(s[kb][i], c, -R.mc)), e1 = fast_exp2(fmaf(s[kb][i + 1], c, -R.mc));
+        ts[0] = kb + i == 0 ? e0 : ts[0] + e0;
+        ts[1] = kb + i == 0 ? e1 : ts[1] + e1;
+        pf[kb * 2 + (i >> 3)][i & 7] = (__bf16)e0;
+        pf[kb * 2 + (i >> 3)][(i & 7) + 1] = (__bf16)e1;
+      }
+  };
+  weights();
+#pragma unroll
+  for (int i = 0; i < 2 * NKB; ++i) asm volatile("" : "+v"(pf[i]));   // rounded here: sunk past the branch, all weights would stay in registers
+  if (__builtin_expect(tile_sum_too_large(ts[0] + ts[1]), 0)) {
+    float mx = s[0][0];
+#pragma unroll
+    for (int kb = 0; kb < NKB; ++kb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[kb][i]);
+    // only rows that need it move, so that no row's bits depend on what its neighbours hold
+    const float over = partner_max(ts[0] + ts[1] <= PACKED_MAX_TILE_SUM ? 0.0f : 1.0f);
+    const float m_new = over > 0.0f ? fmaxf(R.m, partner_max(mx)) : R.m;
+    const float alpha = fast_exp2((R.m - m_new) * c);
+    R.m = m_new;
+    R.mc = packed_mc(m_new, c);
+    R.l *= alpha;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[db][i] *= alpha;
+    weights();
+  }
+  R.l += ts[0] + ts[1];
+}
+// keys of the tile (or step) at t0 that a row with this limit does not see
+template <int NKB>
+__device__ __forceinline__ void packed_mask(f32x16 (&s)[NKB], int valid, int g) {
+  asm volatile("" : "+v"(g));                                     // rare: per-lane constants are not held in registers through the loop
+#pragma unroll
+  for (int kb = 0; kb < NKB; ++kb)
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      if (kb * 32 + 8 * (i >> 2) + 4 * g + (i & 3) >= valid) s[kb][i] = -INFINITY;
+}
+// O^T += V^T P^T over NS16 groups of 16 keys: fragment s16 * NDB + db = 16 keys, channel block db (two transpose reads each), four ahead
+template <int D, int NS16>
+__device__ __forceinline__ void packed_pv(f32x16 (&o)[D / 32], const bf16x8 (&pf)[NS16], unsigned av) {
+  typedef PackedTile<D> C;
+  constexpr int N = NS16 * C::NDB, AHEAD = N < 4 ? N : 4;
+  u32x2 vl[N], vh[N];
+  auto vread = [&](auto i) {
+    constexpr int I = decltype(i)::value, OFF = (I / C::NDB) * 16 * C::ROW_BYTES;
+    const unsigned a = av ^ (unsigned)((I % C::NDB) << 6);
+    read_vt<OFF>(vl[I], a);
+    read_vt<OFF + 8 * C::ROW_BYTES>(vh[I], a);
+  };
+  static_for<0, AHEAD>([&](auto i) { vread(i); });
+  static_for<0, N>([&](auto i) {
+    constexpr int I = decltype(i)::value;
+    wait_lds<2 * (I + AHEAD - 1 < N - 1 ? AHEAD - 1 : N - 1 - I)>();
+    const u32x4 a4 = __builtin_shufflevector(vl[I], vh[I], 0, 1, 2, 3);
+    o[I % C::NDB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a4), pf[I / C::NDB], o[I % C::NDB], 0, 0, 0);
+    if constexpr (I + AHEAD < N) vread(IntC<I + AHEAD>());
+    __builtin_amdgcn_sched_barrier(0);
+  });
+}
+// S^T = K Q^T: fragment NKB * ks + kb = key block kb, k-step ks, four ahead
+template <int D, int NKB>
+__device__ __forceinline__ void packed_qk(f32x16 (&s)[NKB], const bf16x8 (&qf)[D / 16], unsigned ak) {
+  typedef PackedTile<D> C;
+  constexpr int N = NKB * C::NKS;
+  u32x4 kf[N];
+  auto kread = [&](auto i) {
+    constexpr int I = decltype(i)::value;
+    read_k<(I % NKB) * 32 * C::ROW_BYTES>(kf[I], ak ^ (unsigned)((I / NKB) << 5));
+  };
+  static_for<0, 4>([&](auto i) { kread(i); });
+  static_for<0, N>([&](auto i) {
+    constexpr int I = decltype(i)::value, KB = I % NKB, KSTEP = I / NKB;
+    wait_lds<(I + 3 < N - 1 ? 3 : N - 1 - I)>();
+    const f32x16 zero = {};
+    s[KB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[I]), qf[KSTEP], KSTEP == 0 ? zero : s[KB], 0, 0, 0);
+    if constexpr (I + 4 < N) kread(IntC<I + 4>());
+    __builtin_amdgcn_sched_barrier(0);
+  });
+}
+// LDS addresses of this lane's fragments: K row l32, chunk (2 ks + g) ^ swz -> ak ^ (ks << 5); V^T rows 4 g + (lane & 15) / 4 (+ 8, 16 ..), channel
+// block db -> av ^ (db << 6)
+template <int D>
+__device__ __forceinline__ void packed_lds(const char *k, const char *v, int lane, unsigned &ak, unsigned &av) {
+  typedef PackedTile<D> C;
+  const int l32 = lane & 31, g = lane >> 5, rowv = 4 * g + ((lane & 15) >> 2), c0 = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+  ak = (unsigned)(uintptr_t)(const __attribute__((address_space(3))) char *)k + l32 * C::ROW_BYTES + ((g ^ C::swz_k(l32)) << 4);
+  av = (unsigned)(uintptr_t)(const __attribute__((address_space(3))) char *)v + rowv * C::ROW_BYTES + ((c0 ^ C::swz_v(rowv)) << 4) + 8 * (lane & 1);
+}
+// Q^T fragments of a row: lane (l32, g) holds channels 16 ks + 8 g .. + 7
+template <int D>
+__device__ __forceinline__ void packed_load_q(const PackedParams &P, const PackedItem &it, int row, int g, bf16x8 (&qf)[D / 16]) {
+  const int t = packed_div_group(P, row), h = packed_head(it) * P.group + row - t * P.group;
+  const __bf16 *q = P.q + (it.q_base + t) * P.q_tok + h * P.q_head + 8 * g;
+#pragma unroll
+  for (int ks = 0; ks < D / 16; ++ks) qf[ks] = *(const bf16x8 *)(q + ks * 16);
+}
+// Where a row of an item goes: the result, or a plane's share of it.
+template <int D>
+struct PackedTo {
+  __bf16 *out;
+  float *part;         // null: the result
+  float inv;
+};
+// note: this lane also notes the row's maximum and sum, and what the join has to know of the other planes
+template <int D>
+__device__ __forceinline__ PackedTo<D> packed_to(const PackedParams &P, const PackedItem &it, int row, float2 ml, bool note) {
+  const int t = packed_div_group(P, row), h = packed_head(it) * P.group + row - t * P.group, plane = packed_plane(it);
+  const long long id = (long long)(it.q_base + t) * P.n_heads + h;
+  PackedTo<D> to = {nullptr, nullptr, 1.0f};
+  if (plane >= 0) {
+    to.part = P.part_o + ((long long)plane * P.n_rows + id) * D;
+    if (note) {
+      P.part_ml[(long long)plane * P.n_rows + id] = ml;
+      for (int i = 1; i <= packed_missing(it); ++i) P.part_ml[(long long)(plane + i) * P.n_rows + id] = make_float2(-3.0e38f, 0.0f);
+    }
+  } else {
+    to.out = P.out + (it.q_base + t) * P.out_tok + h * P.out_head;
+    to.inv = ml.y > 0.0f ? 1.0f / ml.y : ml.y;                    // no key seen: zeros (a sum that is NaN stays NaN)
+    if (P.planes > 0 && note) P.part_ml[id] = make_float2(0.0f, -1.0f);
+  }
+  return to;
+}
+// eight channels from d0 on
+template <int D>
+__device__ __forceinline__ void packed_put(const PackedTo<D> &to, int d0, const f32x4 &a, const f32x4 &b) {
+  if (to.part) {
+    *(f32x4 *)(to.part + d0) = a;
+    *(f32x4 *)(to.part + d0 + 4) = b;
+    return;
+  }
+  bf16x8 w;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = (__bf16)(a[i] * to.inv), w[i + 4] = (__bf16)(b[i] * to.inv);
+  *(bf16x8 *)(to.out + d0) = w;
+}
+// A wave's O^T (lane = row l32) as rows of LDS.
+template <int D>
+__device__ __forceinline__ void packed_stage(float *row, const f32x16 (&o)[D / 32], int g) {
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int i4 = 0; i4 < 4; ++i4)
+      *(f32x4 *)(row + db * 32 + 8 * i4 + 4 * g) = f32x4{o[db][i4 * 4], o[db][i4 * 4 + 1], o[db][i4 * 4 + 2], o[db][i4 * 4 + 3]};
+}
+
+// ---- a full item: 128 rows, 32 a wave; the waves share every key tile, two stages of tiles copied global -> LDS directly ----
+template <int D>
+__device__ __forceinline__ void packed_full(const PackedItem &it, char *smem, int tid) {
+  typedef PackedTile<D> C;
+  typedef __attribute__((address_space(3))) void *lptr_t;
+  constexpr int WROWS = PF_BK / PACKED_WAVES, NC = WROWS / C::COPY_ROWS;   // tile rows that one wave copies, in so many copies a tensor
+  static_assert(WROWS % 16 == 0, "a wave's rows start at a multiple of the chunk permutations' period");
+  static_assert(C::swz_v(C::COPY_ROWS) == 0 && C::swz_v(2 * C::COPY_ROWS) == 0, "all groups of a wave's rows permute V's chunks alike");
+  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l32 = lane & 31, g = lane >> 5, n_tiles = it.kt1 - it.kt0;
   const int wrow0 = it.row0 + wave * 32;
   const bool has_rows = wrow0 < it.n_rows;
-  const int row = pf_min(wrow0 + l32, it.n_rows - 1);
-  const int limit = packed_limit(P, it, row);
-  const int lim_first = __builtin_amdgcn_readlane(limit, 0), lim_last = __builtin_amdgcn_readlane(limit, 31);
-
-  const int rr = lane / C::CHUNKS, p = lane % C::CHUNKS;
-  const unsigned low_k = (unsigned)((p ^ C::swz_k(rr)) << 4), low_v = (unsigned)((p ^ C::swz_v(rr)) << 4);
+  bf16x8 qf[C::NKS];
+  int pre, prefix_tokens, limit;                                  // the prefix's tiles and keys, if the line has it; this lane's row sees so many own keys
+  float c;
+  {
+    const PackedParams P = packed_params();
+    const int row = pf_min(wrow0 + l32, it.n_rows - 1);
+    packed_load_q<D>(P, it, row, g, qf);                          // first: what waits for it does not wait for the copies behind it
+    pre = packed_has_prefix(it) ? P.prefix_tiles : 0;
+    prefix_tokens = P.prefix_tokens;
+    limit = packed_limit(P, it, row);
+    c = P.scale_log2;
+  }
+  // Copies go by runs of whole tiles (of the prefix, of the line's own keys): from tile to tile only one scalar offset moves on, and a ragged last
+  // tile goes row by row.  With base and offsets worked out for every tile a prompt of 14040 tokens took 757 us instead of 728.
+  __amdgpu_buffer_rsrc_t run_k = __builtin_amdgcn_make_buffer_rsrc(nullptr, 0, 0, 0x00020000u), run_v = run_k;
+  unsigned run_soff = 0, run_tile = 0, run_group = 0, run_vk[NC], run_vv = 0;
+  int run_n = 0;                                                  // tiles left in the run
+  asm volatile("" : "+s"(run_soff), "+s"(run_tile), "+s"(run_group), "+s"(run_n));   // scalars from the start (a zero shared with a vector register would keep them there)
+#pragma unroll
+  for (int i = 0; i < NC; ++i) run_vk[i] = 0;
   char *const mine = smem + wave * (WROWS * C::ROW_BYTES);
   auto copy_tile = [&](int u) __attribute__((always_inline)) {
-    if (u >= n_tiles) return;
     char *to = mine + (u & 1) * C::STAGE_BYTES;
-    const long long e = (long long)u * PF_BK * tok;
-    const __amdgpu_buffer_rsrc_t rk = __builtin_amdgcn_make_buffer_rsrc((void *)(kb + e), 0, -1, 0x00020000u);
-    const __amdgpu_buffer_rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc((void *)(vb + e), 0, -1, 0x00020000u);
-    const int last = it.n_keys - 1 - key0 - u * PF_BK;            // rows past the sequence's end repeat its last key
+    if (__builtin_expect(run_n <= 0, 0)) {
+      if (u >= n_tiles) return;
+      const PackedParams P = packed_params();
+      const PackedKeys K = packed_keys(P, it);
+      const int kt = it.kt0 + u;
+      const bool in_prefix = kt < K.pre;
+      const long long tok = in_prefix ? P.pre_tok : P.kv_tok;
+      const int key0 = (in_prefix ? kt : kt - K.pre) * PF_BK;
+      const int whole = ((in_prefix ? P.prefix_tokens : it.n_keys) - key0) / PF_BK;
+      int lane_l = lane;
+      asm volatile("" : "+v"(lane_l));                            // lane offsets are worked out here, not held in registers through the loop
+      if (whole == 0) {
+        packed_copy<D, false, WROWS>(P, it, K, kt, wave * WROWS, to, lane_l);
+        packed_copy<D, true, WROWS>(P, it, K, kt, wave * WROWS, to + C::TENSOR_BYTES, lane_l);
+        return;
+      }
+      const unsigned rb = (unsigned)(tok * 2);                    // bytes between key rows (below 2^25: checked on the host)
+      run_tile = PF_BK * rb;
+      run_n = __builtin_amdgcn_readfirstlane(pf_min(pf_min(whole, n_tiles - u), 1 << (__builtin_clz(run_tile) - 1)));   // offsets stay below 2^31
+      run_soff = 0;
+      run_group = C::COPY_ROWS * rb;
+      const long long e = (long long)(key0 + wave * WROWS) * tok;
+      run_k = __builtin_amdgcn_make_buffer_rsrc((void *)((in_prefix ? K.k_pre : K.k) + e), 0, -1, 0x00020000u);
+      run_v = __builtin_amdgcn_make_buffer_rsrc((void *)((in_prefix ? K.v_pre : K.v) + e), 0, -1, 0x00020000u);
+      const int rr = lane_l / C::CHUNKS, p = lane_l % C::CHUNKS;
+#pragma unroll
+      for (int i = 0; i < NC; ++i) run_vk[i] = (unsigned)((p ^ C::swz_k(rr) ^ C::swz_k(i * C::COPY_ROWS)) << 4) + (unsigned)rr * rb;
+      run_vv = (unsigned)((p ^ C::swz_v(rr)) << 4) + (unsigned)rr * rb;
+    }
+    --run_n;
     static_for<0, NC>([&](auto gi) {
       constexpr int G = decltype(gi)::value;
-      const unsigned at = (unsigned)pf_min(wave * WROWS + G * C::COPY_ROWS + rr, last) * rb;
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, (lptr_t)(to + G * 1024), 16, at + (low_k ^ (unsigned)(C::swz_k(G * C::COPY_ROWS) << 4)), 0, 0, 0);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, (lptr_t)(to + C::TENSOR_BYTES + G * 1024), 16, at + (low_v ^ (unsigned)(C::swz_v(G * C::COPY_ROWS) << 4)), 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(run_k, (lptr_t)(to + G * 1024), 16, run_vk[G], run_soff + G * run_group, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(run_v, (lptr_t)(to + C::TENSOR_BYTES + G * 1024), 16, run_vv, run_soff + G * run_group, 0, 0);
     });
+    run_soff += run_tile;
   };
   copy_tile(0);
-
-  bf16x8 qf[C::NKS];
-  const int qt = it.q_base + row / P.group, qh = kvh * P.group + row % P.group;
-  {
-    const __bf16 *q = P.q + (long long)qt * P.q_tok + (long long)qh * P.q_head + 8 * g;
+  // the limit grows with the row: the wave's first lane has the least, its 32nd the most
+  const int lim_first = __builtin_amdgcn_readlane(limit, 0), lim_last = __builtin_amdgcn_readlane(limit, 31);
 #pragma unroll
-    for (int ks = 0; ks < C::NKS; ++ks) qf[ks] = *(const bf16x8 *)(q + ks * 16);
-#pragma unroll
-    for (int ks = 0; ks < C::NKS; ++ks) asm volatile("" : "+v"(qf[ks]));   // the compiler waits here, not inside the loop
-  }
+  for (int ks = 0; ks < C::NKS; ++ks) asm volatile("" : "+v"(qf[ks]));   // the compiler waits here, not inside the loop
   f32x16 o[C::NDB];
 #pragma unroll
   for (int db = 0; db < C::NDB; ++db)
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[db][i] = 0.0f;
-  // The reference maximum starts below every score; its multiple is kept finite, so that a masked key's weight against it is 0 and not NaN
-  float m_run = -3.0e38f, l_run = 0.0f, mc = fmaxf(m_run * c, -3.0e38f);
-  const unsigned lds0 = (unsigned)(uintptr_t)(const __attribute__((address_space(3))) char *)smem;
-  const unsigned ak = lds0 + l32 * C::ROW_BYTES + ((g ^ C::swz_k(l32)) << 4);
-  unsigned av;
-  {
-    const int rowv = 4 * g + ((lane & 15) >> 2);
-    const int c0 = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-    av = lds0 + C::TENSOR_BYTES + rowv * C::ROW_BYTES + ((c0 ^ C::swz_v(rowv)) << 4) + 8 * (lane & 1);
-  }
+  PackedRow R = {-3.0e38f, 0.0f, packed_mc(-3.0e38f, c)};
+  unsigned ak, av;
+  packed_lds<D>(smem, smem + C::TENSOR_BYTES, lane, ak, av);
   for (int u = 0; u < n_tiles; ++u) {
     const unsigned stage = (u & 1) * C::STAGE_BYTES;
-    wait_vm<0>();                                            // this wave's share of tile u has landed
+    wait_vm<0>();                                                 // this wave's share of tile u has landed
     __builtin_amdgcn_s_barrier();                                 // ... everyone's has, and everyone is done with tile u-1
     copy_tile(u + 1);
-    const int t0 = key0 + u * PF_BK;
-    if (!has_rows || t0 >= lim_last) continue;                    // none of this wave's rows sees the tile
-    // ---- S^T = K Q^T: fragment 2 ks + kb = key block kb, k-step ks, four ahead ----
+    const int kt = it.kt0 + u, t0 = (kt < pre ? kt : kt - pre) * PF_BK;
+    if (!has_rows || (kt >= pre && t0 >= lim_last)) continue;     // none of this wave's rows sees the tile
     f32x16 s[2];
-    {
-      u32x4 kf[2 * C::NKS];
-      auto kread = [&](auto i) {
-        constexpr int I = decltype(i)::value, KB = I & 1, KSTEP = I >> 1;
-        read_k<KB * 32 * C::ROW_BYTES>(kf[I], (ak + stage) ^ (unsigned)(KSTEP << 5));
-      };
-      static_for<0, 4>([&](auto i) { kread(i); });
-      static_for<0, 2 * C::NKS>([&](auto i) {
-        constexpr int I = decltype(i)::value, KB = I & 1, KSTEP = I >> 1, N = 2 * C::NKS;
-        wait_lds<(I + 3 < N - 1 ? 3 : N - 1 - I)>();
-        const f32x16 zero = {};
-        s[KB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[I]), qf[KSTEP], KSTEP == 0 ? zero : s[KB], 0, 0, 0);
-        if constexpr (I + 4 < N) kread(IntC<I + 4>());
-        __builtin_amdgcn_sched_barrier(0);
-      });
-    }
-    if (__builtin_expect(lim_first - t0 < PF_BK, 0)) {            // some row does not see the whole tile
-      int g_l = g;
-      asm volatile("" : "+v"(g_l));                               // its per-lane constants are not held in registers through the loop
-      const int valid = limit - t0;
-#pragma unroll
-      for (int kb2 = 0; kb2 < 2; ++kb2)
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (kb2 * 32 + 8 * (i >> 2) + 4 * g_l + (i & 3) >= valid) s[kb2][i] = -INFINITY;
-    }
-    // ---- online softmax, one query row per lane ----
+    packed_qk<D, 2>(s, qf, ak + stage);
+    if (__builtin_expect((kt < pre ? prefix_tokens : lim_first) - t0 < PF_BK, 0))   // some row does not see the whole tile
+      packed_mask<2>(s, (kt < pre ? prefix_tokens : limit) - t0, g);
     bf16x8 pf[4];
-    float ts[2];
-    auto weights = [&]() __attribute__((always_inline)) {
-#pragma unroll
-      for (int kb2 = 0; kb2 < 2; ++kb2)
-#pragma unroll
-        for (int i = 0; i < 16; i += 2) {
-          const float e0 = fast_exp2(fmaf(s[kb2][i], c, -mc)), e1 = fast_exp2(fmaf(s[kb2][i + 1], c, -mc));
-          ts[0] = kb2 + i == 0 ? e0 : ts[0] + e0;
-          ts[1] = kb2 + i == 0 ? e1 : ts[1] + e1;
-          pf[kb2 * 2 + (i >> 3)][i & 7] = (__bf16)e0;
-          pf[kb2 * 2 + (i >> 3)][(i & 7) + 1] = (__bf16)e1;
-        }
-    };
-    weights();
-#pragma unroll
-    for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(pf[i]));   // rounded here: sunk past the branch, all 32 weights would stay in registers
-    if (__builtin_expect(tile_sum_too_large(ts[0] + ts[1]), 0)) {
-      float mx = s[0][0];
-#pragma unroll
-      for (int kb2 = 0; kb2 < 2; ++kb2)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[kb2][i]);
-      // only rows that need it move, so that no row's bits depend on what its neighbours hold
-      const float over = partner_max(ts[0] + ts[1] <= PACKED_MAX_TILE_SUM ? 0.0f : 1.0f);
-      const float m_new = over > 0.0f ? fmaxf(m_run, partner_max(mx)) : m_run;
-      const float alpha = fast_exp2((m_run - m_new) * c);
-      m_run = m_new;
-      mc = fmaxf(m_new * c, -3.0e38f);
-      l_run *= alpha;
-#pragma unroll
-      for (int db = 0; db < C::NDB; ++db)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[db][i] *= alpha;
-      weights();
-    }
-    l_run += ts[0] + ts[1];
-    // ---- O^T += V^T P^T: fragment s16 * NDB + db = 16 keys, channel block db (two transpose reads each), four ahead ----
-    {
-      constexpr int N = 4 * C::NDB;
-      u32x2 vl[N], vh[N];
-      auto vread = [&](auto i) {
-        constexpr int I = decltype(i)::value, OFF = (I / C::NDB) * 16 * C::ROW_BYTES;
-        const unsigned a = (av + stage) ^ (unsigned)((I % C::NDB) << 6);
-        read_vt<OFF>(vl[I], a);
-        read_vt<OFF + 8 * C::ROW_BYTES>(vh[I], a);
-      };
-      static_for<0, 4>([&](auto i) { vread(i); });
-      static_for<0, N>([&](auto i) {
-        constexpr int I = decltype(i)::value;
-        wait_lds<2 * (I + 3 < N - 1 ? 3 : N - 1 - I)>();
-        const u32x4 a4 = __builtin_shufflevector(vl[I], vh[I], 0, 1, 2, 3);
-        o[I % C::NDB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a4), pf[I / C::NDB], o[I % C::NDB], 0, 0, 0);
-        if constexpr (I + 4 < N) vread(IntC<I + 4>());
-        __builtin_amdgcn_sched_barrier(0);
-      });
-    }
+    packed_softmax<D, 2>(s, pf, o, R, c);
+    packed_pv<D, 4>(o, pf, av + stage);
   }
-  __syncthreads();
-  // ---- result rows through LDS, so that they are written as full rows ----
-  float *sO = (float *)smem;
-  const float lsum = partner_sum(l_run);
+  // ---- results straight from the accumulators.  A lane holds four channels of every eight, the other half of the wave the other four: pairs
+  // of quads are exchanged, after which a lane has eight channels side by side (16 bytes of the result).  Through LDS, as full rows, this
+  // end of an item took 3 us instead of 1 (two barriers, and eight rounds of address arithmetic per thread). ----
+  if (!has_rows) return;
+  const float lsum = partner_sum(R.l);
+  const bool valid = wrow0 + l32 < it.n_rows;
+  const PackedTo<D> to = packed_to<D>(packed_params(), it, pf_min(wrow0 + l32, it.n_rows - 1), make_float2(R.m, lsum), valid && g == 0);
 #pragma unroll
   for (int db = 0; db < C::NDB; ++db)
 #pragma unroll
-    for (int i4 = 0; i4 < 4; ++i4)
-      *(f32x4 *)(sO + (wave * 32 + l32) * C::LD + db * 32 + 8 * i4 + 4 * g) = f32x4{o[db][i4 * 4], o[db][i4 * 4 + 1], o[db][i4 * 4 + 2], o[db][i4 * 4 + 3]};
-  if (g == 0) s_ml[wave * 32 + l32] = make_float2(m_run, lsum);
-  __syncthreads();
-  const int plane = packed_plane(it), n_valid = pf_min(PACKED_ROWS, it.n_rows - it.row0);
-  for (int e = tid; e < n_valid * (D / 8); e += 256) {
-    const int r = e / (D / 8), d0 = (e % (D / 8)) * 8;
-    const int lr = it.row0 + r, t = it.q_base + lr / P.group, h = kvh * P.group + lr % P.group;
-    const f32x4 a = *(const f32x4 *)(sO + r * C::LD + d0), b = *(const f32x4 *)(sO + r * C::LD + d0 + 4);
-    const float2 ml = s_ml[r];
-    const long long id = (long long)t * P.n_heads + h;
-    if (plane >= 0) {
-      float *po = P.part_o + ((long long)plane * P.n_rows + id) * D + d0;
-      *(f32x4 *)po = a;
-      *(f32x4 *)(po + 4) = b;
-      if (d0 == 0) {
-        P.part_ml[(long long)plane * P.n_rows + id] = ml;
-        for (int i = 1; i <= packed_missing(it); ++i) P.part_ml[(long long)(plane + i) * P.n_rows + id] = make_float2(-3.0e38f, 0.0f);
-      }
-    } else {
-      const float inv = ml.y > 0.0f ? 1.0f / ml.y : ml.y;         // no key seen: zeros (a sum that is NaN stays NaN)
-      bf16x8 w;
+    for (int pair = 0; pair < 2; ++pair) {
+      f32x4 x, y;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = (__bf16)(a[i] * inv), w[i + 4] = (__bf16)(b[i] * inv);
-      *(bf16x8 *)(P.out + (long long)t * P.out_tok + (long long)h * P.out_head + d0) = w;
-      if (P.planes > 0 && d0 == 0) P.part_ml[id] = make_float2(0.0f, -1.0f);
+      for (int i = 0; i < 4; ++i) {
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_int(o[db][pair * 8 + i]), __float_as_int(o[db][pair * 8 + 4 + i]), false, false);
+        x[i] = __int_as_float(r[0]);
+        y[i] = __int_as_float(r[1]);
+      }
+      if (valid) packed_put<D>(to, db * 32 + (2 * pair + g) * 8, x, y);
     }
+}
+
+// ---- a thin item: 32 rows that all waves hold, the keys split over the waves.  Each streams steps of 32 keys through a place of its own in
+// LDS, without barriers: K of the next step is sent once this step's K fragments are in registers, V of the next once its V^T fragments
+// are.  The waves' results are joined in LDS.  For lines of few rows (single tokens), where three waves of a full item would have nothing
+// but copies to do and a tile would take as long. ----
+template <int D>
+__device__ __forceinline__ void packed_thin(const PackedItem &it, char *smem, float2 *s_ml, int tid) {
+  typedef PackedTile<D> C;
+  const PackedParams P = packed_params();
+  constexpr int KEYS = 32, NC = KEYS / C::COPY_ROWS;              // of a step; its copies of one tensor
+  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l32 = lane & 31, g = lane >> 5;
+  const float c = P.scale_log2;
+  const PackedKeys K = packed_keys(P, it);
+  const int row = pf_min(it.row0 + l32, it.n_rows - 1);
+  const int steps = 2 * (it.kt1 - it.kt0), j0 = steps * wave / PACKED_WAVES, j1 = steps * (wave + 1) / PACKED_WAVES;
+  char *mine_k = smem + wave * (2 * KEYS * C::ROW_BYTES), *mine_v = mine_k + KEYS * C::ROW_BYTES;
+  f32x16 o[C::NDB];
+#pragma unroll
+  for (int db = 0; db < C::NDB; ++db)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[db][i] = 0.0f;
+  PackedRow R = {-3.0e38f, 0.0f, packed_mc(-3.0e38f, c)};
+  if (j0 < j1) {
+    bf16x8 qf[C::NKS];
+    packed_load_q<D>(P, it, row, g, qf);
+    packed_copy<D, false, KEYS>(P, it, K, it.kt0 + j0 / 2, j0 % 2 * KEYS, mine_k, lane);
+    packed_copy<D, true, KEYS>(P, it, K, it.kt0 + j0 / 2, j0 % 2 * KEYS, mine_v, lane);
+    const int limit = packed_limit(P, it, row), lim_first = __builtin_amdgcn_readlane(limit, 0);
+#pragma unroll
+    for (int ks = 0; ks < C::NKS; ++ks) asm volatile("" : "+v"(qf[ks]));
+    unsigned ak, av;
+    packed_lds<D>(mine_k, mine_v, lane, ak, av);
+    for (int j = j0; j < j1; ++j) {
+      const bool more = j + 1 < j1;
+      const int kt = it.kt0 + j / 2, t0 = (kt < K.pre ? kt : kt - K.pre) * PF_BK + j % 2 * KEYS;
+      wait_vm<NC>();                                              // K of this step has landed (its V may still travel)
+      f32x16 s[1];
+      packed_qk<D, 1>(s, qf, ak);
+      if (more) packed_copy<D, false, KEYS>(P, it, K, it.kt0 + (j + 1) / 2, (j + 1) % 2 * KEYS, mine_k, lane);
+      if (__builtin_expect((kt < K.pre ? P.prefix_tokens : lim_first) - t0 < KEYS, 0))
+        packed_mask<1>(s, (kt < K.pre ? P.prefix_tokens : limit) - t0, g);
+      bf16x8 pf[2];
+      packed_softmax<D, 1>(s, pf, o, R, c);
+      if (more) wait_vm<NC>();                                    // V of this step has landed (K of the next may still travel)
+      else wait_vm<0>();
+      packed_pv<D, 2>(o, pf, av);
+      if (more) packed_copy<D, true, KEYS>(P, it, K, it.kt0 + (j + 1) / 2, (j + 1) % 2 * KEYS, mine_v, lane);
+    }
+  }
+  __syncthreads();
+  float *sO = (float *)smem;
+  const float lsum = partner_sum(R.l);
+  packed_stage<D>(sO + (wave * 32 + l32) * C::LD, o, g);
+  if (g == 0) s_ml[wave * 32 + l32] = make_float2(R.m, lsum);
+  __syncthreads();
+  for (int e = tid; e < 32 * (D / 8); e += PACKED_WAVES * 64) {
+    const int r = e / (D / 8), d0 = (e % (D / 8)) * 8;
+    float2 ml[PACKED_WAVES], all = make_float2(-3.0e38f, 0.0f);
+#pragma unroll
+    for (int w = 0; w < PACKED_WAVES; ++w) ml[w] = s_ml[w * 32 + r], all.x = fmaxf(all.x, ml[w].x);
+    f32x4 a = {0.0f, 0.0f, 0.0f, 0.0f}, b = a;
+#pragma unroll
+    for (int w = 0; w < PACKED_WAVES; ++w) {
+      const float f = fast_exp2((ml[w].x - all.x) * c);
+      const f32x4 x = *(const f32x4 *)(sO + (w * 32 + r) * C::LD + d0), y = *(const f32x4 *)(sO + (w * 32 + r) * C::LD + d0 + 4);
+      all.y += f * ml[w].y;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) a[i] += f * x[i], b[i] += f * y[i];
+    }
+    if (it.row0 + r < it.n_rows) packed_put<D>(packed_to<D>(P, it, it.row0 + r, all, d0 == 0), d0, a, b);
   }
 }
 
-// Joins the planes of every row: out = sum_p 2^((m_p - M) c) O_p / sum_p 2^((m_p - M) c) l_p, planes in order.
 template <int D>
-__global__ __launch_bounds__(256) void pf_packed_join_kernel(PackedParams P) {
-  constexpr int LANES = D / 8;                                    // of a row, eight channels each
-  const long long id = (long long)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
+__global__ __launch_bounds__(PACKED_WAVES * 64, 2 * 128 / D) void pf_packed_attn_kernel(PackedParams) {
+  typedef PackedTile<D> C;
+  constexpr int THIN_STAGE = PACKED_WAVES * 32 * C::LD * 4;       // where a thin item joins its waves' results
+  __shared__ __attribute__((aligned(1024))) char smem[2 * C::STAGE_BYTES > THIN_STAGE ? 2 * C::STAGE_BYTES : THIN_STAGE];
+  __shared__ float2 s_ml[PACKED_WAVES * 32];
+  // the plan was written before this launch and is constant during it: scalar loads, so that what follows from an item is scalar too
+  struct Words {
+    unsigned long long w[sizeof(PackedItem) / 8];
+  } words;
+  const auto *from = (const __attribute__((address_space(4))) unsigned long long *)(packed_params().items + blockIdx.x);
+#pragma unroll
+  for (int i = 0; i < (int)(sizeof(PackedItem) / 8); ++i) words.w[i] = from[i];
+  const PackedItem it = __builtin_bit_cast(PackedItem, words);
+  if (packed_is_thin(it)) packed_thin<D>(it, smem, s_ml, threadIdx.x);
+  else packed_full<D>(it, smem, threadIdx.x);
+}
+
+// Joins the planes of every row: out = sum_p 2^((m_p - M) c) O_p / sum_p 2^((m_p - M) c) l_p.
+//
+// Few planes: D / 8 lanes take a row, eight channels each, plane after plane.
+template <int D>
+__global__ __launch_bounds__(256) void pf_packed_join_few_kernel(PackedParams P) {
+  constexpr int LANES = D / 8;
+  const int id = blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
   if (id >= P.n_rows) return;
   const int d0 = threadIdx.x % LANES * 8;
-  const float2 first = P.part_ml[id];
-  if (first.y == -1.0f) return;                                   // written by its only item
-  float top = first.x;
-  for (int p = 1; p < P.planes; ++p) top = fmaxf(top, P.part_ml[(long long)p * P.n_rows + id].x);
-  float acc[8] = {}, sum = 0.0f;
-  for (int p = 0; p < P.planes; ++p) {
-    const float2 ml = P.part_ml[(long long)p * P.n_rows + id];
-    if (ml.y == 0.0f) continue;                                   // saw no key (nothing was written for a plane without an item)
-    const float w = fast_exp2((ml.x - top) * P.scale_log2);
-    sum += w * ml.y;
-    const float *o = P.part_o + ((long long)p * P.n_rows + id) * D + d0;
-    const f32x4 a = *(const f32x4 *)o, b = *(const f32x4 *)(o + 4);
+  float2 ml[PACKED_FEW_PLANES];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) acc[i] += w * a[i], acc[i + 4] += w * b[i];
+  for (int p = 0; p < PACKED_FEW_PLANES; ++p) ml[p] = p < P.planes ? P.part_ml[(long long)p * P.n_rows + id] : make_float2(-3.0e38f, 0.0f);
+  if (ml[0].y == -1.0f) return;                                   // written by its only item
+  float top = ml[0].x, sum = 0.0f, acc[8] = {};
+#pragma unroll
+  for (int p = 1; p < PACKED_FEW_PLANES; ++p) top = fmaxf(top, ml[p].x);
+  f32x4 x[PACKED_FEW_PLANES][2];
+#pragma unroll
+  for (int p = 0; p < PACKED_FEW_PLANES; ++p) {
+    x[p][0] = x[p][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    if (ml[p].y == 0.0f) continue;                                // a plane that saw no key (or has no item) counts nothing
+    const float *o = P.part_o + ((long long)p * P.n_rows + id) * D + d0;
+    x[p][0] = *(const f32x4 *)o;
+    x[p][1] = *(const f32x4 *)(o + 4);
+  }
+#pragma unroll
+  for (int p = 0; p < PACKED_FEW_PLANES; ++p) {
+    if (ml[p].y == 0.0f) continue;
+    const float w = fast_exp2((ml[p].x - top) * P.scale_log2);
+    sum += w * ml[p].y;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[e] += w * x[p][0][e], acc[e + 4] += w * x[p][1][e];
   }
   const float inv = sum > 0.0f ? 1.0f / sum : sum;
-  bf16x8 w;
+  bf16x8 r;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) w[i] = (__bf16)(acc[i] * inv);
-  *(bf16x8 *)(P.out + id / P.n_heads * P.out_tok + id % P.n_heads * P.out_head + d0) = w;
+  for (int i = 0; i < 8; ++i) r[i] = (__bf16)(acc[i] * inv);
+  *(bf16x8 *)(P.out + id / P.n_heads * P.out_tok + id % P.n_heads * P.out_head + d0) = r;
+}
+// Many planes: a wave takes a row: its lanes look at a
+// plane's maximum and sum each, then groups of D / 8 lanes (eight channels a lane) add up every 64 / (D / 8)-th plane and the groups'
+// sums are added in a fixed order.  Bound: with few rows two round trips to memory, with many the planes' bytes.
+__device__ __forceinline__ float packed_lane(float x, int lane) { return __int_as_float(__builtin_amdgcn_ds_bpermute(lane * 4, __float_as_int(x))); }
+template <int D>
+__global__ __launch_bounds__(256) void pf_packed_join_kernel(PackedParams P) {
+  constexpr int LANES = D / 8, GROUPS = 64 / LANES;
+  const int lane = threadIdx.x & 63;
+  const int id = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (id >= P.n_rows) return;
+  const int d0 = lane % LANES * 8, grp = lane / LANES;
+  float2 ml[PACKED_JOIN_BATCHES];
+  float top = -3.0e38f;
+#pragma unroll
+  for (int b = 0; b < PACKED_JOIN_BATCHES; ++b) {
+    ml[b] = make_float2(-3.0e38f, 0.0f);
+    if (b * 64 + lane < P.planes) ml[b] = P.part_ml[(long long)(b * 64 + lane) * P.n_rows + id];
+  }
+  if (__builtin_amdgcn_readfirstlane(__float_as_int(ml[0].y)) == __float_as_int(-1.0f)) return;   // written by its only item
+#pragma unroll
+  for (int b = 0; b < PACKED_JOIN_BATCHES; ++b) top = fmaxf(top, ml[b].x);
+#pragma unroll
+  for (int step = 1; step < 64; step *= 2) top = fmaxf(top, packed_lane(top, lane ^ step));
+  float w[PACKED_JOIN_BATCHES], sum = 0.0f;
+#pragma unroll
+  for (int b = 0; b < PACKED_JOIN_BATCHES; ++b) {
+    w[b] = ml[b].y == 0.0f ? 0.0f : fast_exp2((ml[b].x - top) * P.scale_log2);   // a plane that saw no key (or has no item) counts nothing
+    sum += w[b] * ml[b].y;
+  }
+#pragma unroll
+  for (int step = 1; step < 64; step *= 2) sum += packed_lane(sum, lane ^ step);
+  float acc[8] = {};
+#pragma unroll
+  for (int b = 0; b < PACKED_JOIN_BATCHES; ++b) {
+    for (int p0 = 0; p0 < 64 && b * 64 + p0 < P.planes; p0 += 2 * GROUPS) {
+      f32x4 x[2][2];
+      float f[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {                               // two planes of every group in flight
+        const int p = p0 + i * GROUPS + grp;
+        f[i] = packed_lane(w[b], pf_min(p, 63));
+        if (p > 63) f[i] = 0.0f;
+        x[i][0] = x[i][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        if (f[i] != 0.0f) {
+          const float *o = P.part_o + ((long long)(b * 64 + p) * P.n_rows + id) * D + d0;
+          x[i][0] = *(const f32x4 *)o;
+          x[i][1] = *(const f32x4 *)(o + 4);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] += f[i] * x[i][0][e], acc[e + 4] += f[i] * x[i][1][e];
+    }
+  }
+#pragma unroll
+  for (int step = LANES; step < 64; step *= 2)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[e] += packed_lane(acc[e], lane ^ step);
+  if (grp != 0) return;
+  const float inv = sum > 0.0f ? 1.0f / sum : sum;
+  bf16x8 r;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) r[i] = (__bf16)(acc[i] * inv);
+  *(bf16x8 *)(P.out + id / P.n_heads * P.out_tok + id % P.n_heads * P.out_head + d0) = r;
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------
@@ -346,64 +693,222 @@ struct PackedPlan {
   int planes = 0;
 };
 
-// Key tiles per item: where whole row tiles are fewer than the places that workgroups find on the chip, their keys are cut until about as
-// many items are there.
-static constexpr int PACKED_PLACES = 512, PACKED_MIN_SEG = 8;
+// Rows that share their keys: one sequence's, or in front of the prefix those of neighbouring sequences.
+struct PackedLine {
+  int q_base, n_rows, k_base, n_keys;
+  bool prefix;                 // has the prefix's tiles
+  int stack;                   // >= 0: the line that has the prefix in this one's place; -1: this line has all of its rows' keys; -2: it is such a line
+  bool thin() const { return n_rows <= PACKED_THIN_ROWS; }
+};
+struct PackedRowTile {
+  int line, row0, n_kt;
+  bool thin;
+  int load;                    // its time, where all places are taken, in key tiles of a full item
+};
 
-static void packed_cut(PackedPlan &plan, PackedItem it, int n_kt, int seg, int first_plane, int planes_of_line, bool alone) {
-  const int n = std::max(1, pf_ceil_div(n_kt, seg));
-  for (int i = 0; i < n; ++i) {
-    PackedItem x = it;
-    x.kt0 = pf_seg_begin(n_kt, n, i);
-    x.kt1 = pf_seg_begin(n_kt, n, i + 1);
-    if (!(alone && n == 1)) {
-      x.head |= (first_plane + i + 1) << 13;
-      if (i == n - 1) x.head |= (planes_of_line - n) << 22;
-    }
-    plan.items.push_back(x);
+// What the planner knows of the time that things take, in microseconds, measured on launches of 32 to 1024 items of 1 to 32 key tiles.  All
+// places taken: a full item's key tile, and a key tile that no other row tile reads from memory; few taken: a key tile of a full and of a thin item.
+// An item's set-up and end; the second launch; a row of a plane written and read.
+struct PackedCosts {
+  int places;
+  double tile, tile_alone, tile_few, tile_thin, item, join, plane_row;
+};
+static PackedCosts packed_costs(int head_dim) {
+  if (head_dim == 128) return {512, 1.95, 3.4, 1.15, 0.42, 3.0, 6.0, 2.3e-4};
+  return {1024, 2.3, 3.4, 0.85, 0.32, 3.0, 6.0, 1.2e-4};
+}
+
+static int packed_line_tiles(const pf_packed *p, const PackedLine &l, int row0, int pre_kt) {
+  const int G = p->n_heads / p->n_kv_heads, last = pf_min(row0 + PACKED_ROWS, l.n_rows) - 1;
+  const int own = l.n_keys > 0 ? pf_ceil_div(packed_host_limit(p, l.n_rows / G, l.n_keys, last / G), PF_BK) : 0;
+  return own + (l.prefix ? pre_kt : 0);
+}
+
+// How a batch's row tiles (heaviest first) are cut: the first `whole` not at all, the others into runs of at most seg full key tiles' time.
+struct PackedCut {
+  int whole, seg;
+  int of(int i, const PackedRowTile &t) const { return i < whole ? 1 : std::max(1, std::min(pf_ceil_div(t.load, seg), t.n_kt)); }
+};
+
+// Time that the launch takes under a cut; more than `limit` is not worked out.
+static double packed_time(const std::vector<PackedRowTile> &tiles, int heads, const PackedCut &cut, const PackedCosts &C, double limit) {
+  long long n = 0;
+  int longest = 0;
+  double work = 0.0, few = 0.0;
+  for (size_t i = 0; i < tiles.size(); ++i) {
+    const int cuts = cut.of((int)i, tiles[i]);
+    n += (long long)cuts * heads;
+    longest = std::max(longest, pf_ceil_div(tiles[i].load, cuts));
+    few = std::max(few, pf_ceil_div(tiles[i].n_kt, cuts) * (tiles[i].thin ? C.tile_thin : C.tile_few));
+    work += tiles[i].load * (double)heads;
   }
+  if (n <= C.places / 2) return C.item + few;
+  if ((work * C.tile + n * C.item) / C.places > limit) return 1e300;
+  std::vector<int> count(longest + 1, 0);
+  for (size_t i = 0; i < tiles.size(); ++i) {
+    const int cuts = cut.of((int)i, tiles[i]);
+    count[pf_ceil_div(tiles[i].load, cuts)] += cuts * heads;      // (a run may be a tile shorter)
+  }
+  // heaviest first, each to the place that is free first
+  std::priority_queue<double, std::vector<double>, std::greater<double>> free_at;
+  for (int i = 0; i < C.places; ++i) free_at.push(0.0);
+  double end = C.item + few;
+  for (int t = longest; t >= 0; --t)
+    for (int i = 0; i < count[t]; ++i) {
+      const double at = free_at.top() + C.item + t * C.tile;
+      free_at.pop();
+      free_at.push(at);
+      end = std::max(end, at);
+      if (end > limit) return 1e300;
+    }
+  return end;
+}
+
+// The batch's lines and how their keys are cut, as fast as the costs above say.  take_all: every sequence has the prefix in its own line;
+// otherwise those whose tiles would stay mostly empty in front of it are stacked.  Returns the time.
+struct PackedLayout {
+  std::vector<PackedLine> lines;
+  std::vector<PackedRowTile> tiles;
+  int planes = 0;
+};
+static double packed_lay_out(const pf_packed *p, bool take_all, PackedLayout &L, std::vector<int> &cuts, std::vector<int> &first) {
+  const int G = p->n_heads / p->n_kv_heads, KV = p->n_kv_heads, BQ = PACKED_ROWS;
+  const int pre_kt = pf_ceil_div(p->prefix_tokens, PF_BK);
+  const PackedCosts C = packed_costs(p->head_dim);
+  std::vector<PackedLine> &lines = L.lines;
+  std::vector<PackedRowTile> &tiles = L.tiles;
+  int stack = -1;
+  bool any_stack = false;
+  for (int s = 0; s < p->n_seqs; ++s) {
+    const int lq = p->cu_q[s + 1] - p->cu_q[s], r = lq * G;
+    if (lq == 0) continue;
+    // the rows that its tiles would leave empty in front of the prefix, against parking its rows' partial results
+    const double empty = r <= PACKED_THIN_ROWS ? 1.0 : pf_ceil_div(r, BQ) - (double)r / BQ;
+    const bool own = pre_kt == 0 || take_all || empty * pre_kt * C.tile / C.places < 2.0 * r * C.plane_row;
+    if (own) {
+      stack = -1;
+    } else {
+      if (stack < 0) {
+        stack = (int)lines.size();
+        lines.push_back({p->cu_q[s], 0, 0, 0, true, -2});
+      }
+      lines[stack].n_rows += r;
+      any_stack = true;
+    }
+    lines.push_back({p->cu_q[s], r, p->cu_k[s], p->cu_k[s + 1] - p->cu_k[s], pre_kt > 0 && own, stack});
+  }
+  long long rows = 0, with_prefix = 0;
+  for (const PackedLine &l : lines)
+    if (l.prefix) with_prefix += pf_ceil_div(l.n_rows, BQ);
+  // a key tile's time in full tiles: what its bytes take where row tiles that read them are few, if that is more
+  auto load_of = [&](int n_pre, int n_own, const PackedLine &l) {
+    const double least = l.thin() ? C.tile_thin / C.tile_few : 1.0, alone = C.tile_alone / C.tile;
+    const double pre = std::max(least, alone / std::max(1ll, with_prefix)), own = std::max(least, alone / pf_ceil_div(l.n_rows, BQ));
+    return (int)ceil(n_pre * pre + n_own * own - 1e-9);
+  };
+  for (size_t l = 0; l < lines.size(); ++l)
+    for (int r0 = 0; r0 < lines[l].n_rows; r0 += BQ) {
+      const int n_kt = packed_line_tiles(p, lines[l], r0, pre_kt), pre = lines[l].prefix ? pre_kt : 0;
+      tiles.push_back({(int)l, r0, n_kt, lines[l].thin(), load_of(pre, n_kt - pre, lines[l])});
+      if (lines[l].stack != -2) rows += pf_min(BQ, lines[l].n_rows - r0);
+    }
+  std::stable_sort(tiles.begin(), tiles.end(), [](const PackedRowTile &a, const PackedRowTile &b) { return a.load > b.load; });
+  const int longest = tiles.empty() ? 1 : std::max(1, tiles[0].load);
+  // A row's planes: its stacked line's first, then its own line's (every tile of a stacked line is cut alike, so that own planes start at one place).
+  auto stack_cuts = [&](int line, int seg) { return std::max(1, std::min(pf_ceil_div(load_of(pre_kt, 0, lines[line]), seg), pre_kt)); };
+  auto cuts_of = [&](const PackedCut &cut, size_t i) {
+    return lines[tiles[i].line].stack == -2 ? stack_cuts(tiles[i].line, cut.seg) : cut.of((int)i, tiles[i]);
+  };
+  auto planes_of = [&](const PackedCut &cut, double *parked) {
+    int most = 0;
+    *parked = 0.0;
+    for (size_t i = 0; i < tiles.size(); ++i) {
+      const PackedLine &l = lines[tiles[i].line];
+      const int n = cuts_of(cut, i), before = l.stack >= 0 ? stack_cuts(l.stack, cut.seg) : 0;
+      if (l.stack == -1 && n == 1) continue;
+      most = std::max(most, before + n);
+      *parked += (double)n * pf_min(BQ, l.n_rows - tiles[i].row0);
+    }
+    return most;
+  };
+  PackedCut best = {0, longest};
+  double parked = 0.0, least = 1e300;
+  if ((long long)tiles.size() * KV <= 8ll * C.places) {
+    const int rounds = (int)((long long)tiles.size() * KV / C.places);
+    for (int whole_rounds = any_stack ? 0 : rounds; whole_rounds >= 0; whole_rounds = whole_rounds > 0 ? 0 : -1) {
+      const int whole = whole_rounds * C.places / KV;
+      const int most = whole < (int)tiles.size() ? std::max(1, tiles[whole].load) : 1;   // the longest that is cut
+      for (int n : {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 40, 48, 64, 80, 96, 120}) {
+        const PackedCut cut = {whole, pf_ceil_div(most, n)};
+        const int planes = planes_of(cut, &parked);
+        if (planes > PACKED_MAX_PLANES || (n > 1 && (double)planes * rows * KV * (p->head_dim * 4 + 8) > 1e9)) break;
+        const double rest = planes ? C.join + parked * KV * C.plane_row : 0.0;
+        if (rest >= least) break;
+        // a plan with partial results has to be a good deal faster: whole launches run at their power limit, where idle places at the end
+        // leave the others a higher clock
+        const double t = (packed_time(tiles, KV, cut, C, least) + rest) * (planes && !any_stack ? 1.1 : 1.0);
+        if (t < least) {
+          least = t;
+          best = cut;
+        }
+        if (cut.seg == 1) break;
+      }
+    }
+  } else {
+    double work = 0.0;
+    for (const PackedRowTile &t : tiles) work += (double)t.load * KV;
+    least = work * C.tile / C.places;
+  }
+  L.planes = planes_of(best, &parked);
+  for (size_t i = 0; i < tiles.size(); ++i) {
+    const int st = lines[tiles[i].line].stack;
+    cuts.push_back(cuts_of(best, i));
+    first.push_back(st >= 0 ? stack_cuts(st, best.seg) : 0);
+  }
+  return least;
 }
 
 static void packed_make(const pf_packed *p, PackedPlan &plan) {
-  const int G = p->n_heads / p->n_kv_heads, KV = p->n_kv_heads, BQ = PACKED_ROWS;
-  const long long total_rows = (long long)p->cu_q[p->n_seqs] * G;
-  const int pre_kt = pf_ceil_div(p->prefix_tokens, PF_BK);
-  // the work in key tiles, the longest line
-  long long work = (total_rows + BQ - 1) / BQ * pre_kt, longest = pre_kt;
-  for (int s = 0; s < p->n_seqs; ++s) {
-    const int lq = p->cu_q[s + 1] - p->cu_q[s], lk = p->cu_k[s + 1] - p->cu_k[s];
-    const long long rows = (long long)lq * G;
-    for (long long r0 = 0; r0 < rows; r0 += BQ)
-      work += pf_ceil_div(packed_host_limit(p, lq, lk, (int)((std::min(r0 + BQ, rows) - 1) / G)), PF_BK);
-    longest = std::max<long long>(longest, pf_ceil_div(lk, PF_BK));
+  PackedLayout L, all;
+  std::vector<int> cuts, first, cuts_all, first_all;
+  double t = packed_lay_out(p, false, L, cuts, first);
+  if (L.planes > 0 && p->prefix_tokens > 0 && packed_lay_out(p, true, all, cuts_all, first_all) < t) {
+    L = std::move(all);
+    cuts.swap(cuts_all);
+    first.swap(first_all);
   }
-  work *= KV;
-  const int seg = (int)std::max<long long>(std::max<long long>(PACKED_MIN_SEG, (work + PACKED_PLACES - 1) / PACKED_PLACES), (longest + 120) / 120);
-  const int pre_planes = pre_kt ? pf_ceil_div(pre_kt, seg) : 0;
-  int own_planes = 0;
-  for (int s = 0; s < p->n_seqs; ++s) {
-    const int lq = p->cu_q[s + 1] - p->cu_q[s], lk = p->cu_k[s + 1] - p->cu_k[s];
-    if (lq > 0) own_planes = std::max(std::max(own_planes, 1), pf_ceil_div(pf_ceil_div(packed_host_limit(p, lq, lk, lq - 1), PF_BK), seg));
-  }
-  if (pre_planes == 0 && own_planes <= 1) own_planes = 0;
-  plan.planes = pre_planes + own_planes;
-  for (long long r0 = 0; pre_kt && r0 < total_rows; r0 += BQ)
-    for (int h = 0; h < KV; ++h) {
-      const PackedItem it = {0, (int)r0, (int)total_rows, 0, p->prefix_tokens, 0, 0, h | 1 << PACKED_PREFIX_BIT};
-      packed_cut(plan, it, pre_kt, seg, 0, pre_planes, false);
-    }
-  for (int s = 0; s < p->n_seqs; ++s) {
-    const int lq = p->cu_q[s + 1] - p->cu_q[s], lk = p->cu_k[s + 1] - p->cu_k[s];
-    const int rows = lq * G;
-    for (int r0 = 0; r0 < rows; r0 += BQ) {
-      const int n_kt = pf_ceil_div(packed_host_limit(p, lq, lk, (pf_min(r0 + BQ, rows) - 1) / G), PF_BK);
-      for (int h = 0; h < KV; ++h) {
-        const PackedItem it = {p->cu_q[s], r0, rows, p->cu_k[s], lk, 0, 0, h};
-        packed_cut(plan, it, n_kt, seg, pre_planes, own_planes, pre_planes == 0);
+  plan.planes = L.planes;
+  struct Loaded {
+    PackedItem item;
+    int load;
+  };
+  std::vector<Loaded> items;
+  for (int h = 0; h < p->n_kv_heads; ++h)
+    for (size_t t = 0; t < L.tiles.size(); ++t) {
+      const PackedRowTile &tile = L.tiles[t];
+      const PackedLine &l = L.lines[tile.line];
+      const int n = cuts[t];
+      for (int i = 0; i < n; ++i) {
+        PackedItem it = {l.q_base, tile.row0, l.n_rows, l.k_base, l.n_keys, pf_seg_begin(tile.n_kt, n, i), pf_seg_begin(tile.n_kt, n, i + 1), h};
+        if (l.prefix) it.head |= 1 << PACKED_PREFIX_BIT;
+        if (tile.thin) it.head |= (int)(1u << 31);
+        if (!(l.stack == -1 && n == 1)) {
+          it.head |= (first[t] + i + 1) << 13;
+          if (i == n - 1 && l.stack != -2) it.head |= (L.planes - first[t] - n) << 22;
+        }
+        items.push_back({it, tile.load / n});
       }
     }
+  // Heaviest first.  Workgroup i runs on die i % 8, and every die has an L2 of its own: among items of one load, which have no order to keep,
+  // the heads are dealt out to the dies in runs, so that a die's workgroups read the keys of one head or two.
+  std::stable_sort(items.begin(), items.end(), [](const Loaded &a, const Loaded &b) { return a.load > b.load; });
+  plan.items.resize(items.size());
+  for (size_t a = 0, b; a < items.size(); a = b) {
+    for (b = a + 1; b < items.size() && items[b].load == items[a].load;) ++b;
+    size_t from = a;
+    for (size_t d = 0; d < PF_NUM_XCD; ++d)
+      for (size_t i = a + (d + PF_NUM_XCD - a % PF_NUM_XCD) % PF_NUM_XCD; i < b; i += PF_NUM_XCD) plan.items[i] = items[from++].item;
   }
-  std::stable_sort(plan.items.begin(), plan.items.end(), [](const PackedItem &a, const PackedItem &b) { return a.kt1 - a.kt0 > b.kt1 - b.kt0; });
 }
 
 static size_t packed_part_bytes(const pf_packed *p, int planes) {
@@ -501,7 +1006,17 @@ extern "C" int pf_packed_attn_fwd(const pf_packed *packed, const void *q, const 
   P.n_heads = packed->n_heads;
   P.group = packed->n_heads / packed->n_kv_heads;
   P.block = packed->block;
+  {
+    // with 2^(s-1) < group <= 2^s and mul = ceil(2^(31+s) / group) < 2^32 the quotient is exact for n < 2^31: mul * group exceeds 2^(31+s) by
+    // less than group <= 2^s, and n times that by less than 2^(31+s)
+    int s = 0;
+    while ((1 << s) < P.group) ++s;
+    P.group_mul = (unsigned)(((1ull << (31 + s)) + P.group - 1) / P.group);
+    P.group_shift = s > 0 ? s - 1 : 0;
+  }
   P.planes = packed->n_planes;
+  P.prefix_tokens = packed->prefix_tokens;
+  P.prefix_tiles = pf_ceil_div(packed->prefix_tokens, PF_BK);
   P.part_o = (float *)workspace;
   P.part_ml = (float2 *)((char *)workspace + (size_t)P.planes * P.n_rows * D * 4);
   P.q_tok = q_layout ? q_layout->token_stride : D;
@@ -515,14 +1030,17 @@ extern "C" int pf_packed_attn_fwd(const pf_packed *packed, const void *q, const 
   const float scale = softmax_scale > 0.0f ? softmax_scale : 1.0f / sqrtf((float)D);
   P.scale_log2 = scale * 1.4426950408889634f;
   hipStream_t st = (hipStream_t)stream;
-  if (D == 128) hipLaunchKernelGGL((pf_packed_attn_kernel<128>), dim3(packed->n_items), dim3(256), 0, st, P);
-  else hipLaunchKernelGGL((pf_packed_attn_kernel<64>), dim3(packed->n_items), dim3(256), 0, st, P);
+  const dim3 grid(packed->n_items), block(PACKED_WAVES * 64);
+  if (D == 128) hipLaunchKernelGGL((pf_packed_attn_kernel<128>), grid, block, 0, st, P);
+  else hipLaunchKernelGGL((pf_packed_attn_kernel<64>), grid, block, 0, st, P);
   PF_HIP_CHECK(hipGetLastError());
   if (P.planes > 0) {
-    const int rows = 256 / (D / 8);
-    const dim3 grid((unsigned)((P.n_rows + rows - 1) / rows));
-    if (D == 128) hipLaunchKernelGGL((pf_packed_join_kernel<128>), grid, dim3(256), 0, st, P);
-    else hipLaunchKernelGGL((pf_packed_join_kernel<64>), grid, dim3(256), 0, st, P);
+    const bool few = P.planes <= PACKED_FEW_PLANES;
+    const dim3 rows((unsigned)pf_ceil_div(P.n_rows, few ? 256 / (D / 8) : 4));
+    if (D == 128 && few) hipLaunchKernelGGL((pf_packed_join_few_kernel<128>), rows, block, 0, st, P);
+    else if (D == 128) hipLaunchKernelGGL((pf_packed_join_kernel<128>), rows, block, 0, st, P);
+    else if (few) hipLaunchKernelGGL((pf_packed_join_few_kernel<64>), rows, block, 0, st, P);
+    else hipLaunchKernelGGL((pf_packed_join_kernel<64>), rows, block, 0, st, P);
     PF_HIP_CHECK(hipGetLastError());
   }
   return PF_OK;
