@@ -415,8 +415,9 @@ size_t pf_packed_workspace_bytes(const pf_packed *packed);
  *   k_prefix, v_prefix  dev [n_kv_heads][prefix_tokens][head_dim] or by prefix_layout; NULL without a prefix
  *   softmax_scale       0 = 1/sqrt(head_dim)
  *   workspace           dev, >= pf_packed_workspace_bytes, 16-byte aligned
- * 16-byte aligned tensors; a NULL layout = packed per head.  Launches that share a workspace must not overlap in time; the
- * plan is only read.
+ * 16-byte aligned tensors; a NULL layout = packed per head.  The plan (it holds arrival counters) and the workspace are
+ * written by the launch and left ready for the next one: launches that share either must not overlap in time (same
+ * stream, or ordered by events).
  */
 int pf_packed_attn_fwd(const pf_packed *packed, const void *q, const pf_chunk_layout *q_layout, const void *k, const void *v,
                        const pf_chunk_layout *kv_layout, const void *k_prefix, const void *v_prefix,

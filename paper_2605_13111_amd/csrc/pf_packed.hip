@@ -10,8 +10,8 @@
 // of few rows (single tokens) would each read the prefix for a tile of which they fill little: in front of the prefix they are stacked,
 // neighbours in one line, and each has its own keys as another line.  A work item is a tile of rows against a run of key tiles of its
 // line: the host cuts the work into items and orders them (pf_packed_plan), heaviest first.  Rows whose keys are cut into several items
-// park unnormalised partial results (O, m, l) in fp32, one plane per item, row by row; a second kernel joins them in a fixed order.  A
-// launch boundary stands between: no counters, no waiting.
+// park unnormalised partial results (O, m, l) in fp32, one plane per item, row by row, and they are joined plane by plane in a fixed
+// order: by a second kernel, or, where a head has a few rows only, by the head's last workgroup to finish (no spinning).
 //
 // Scores, softmax and value products as in the ragged-cache kernels: S^T = K Q^T and O^T += V^T P^T on 32x32x16 bf16 MFMAs with fp32
 // accumulation, one query row per lane; weights are rounded to bf16 for the second product (2^-8 relative at most each, the sum is
@@ -24,6 +24,9 @@
 #include <queue>
 #include <vector>
 #include "pf_packed_steps.h"
+#ifndef PF_STRICT_FENCES
+#define PF_STRICT_FENCES 0   // 1: release and acquire fences around the arrival counters (the memory model's own form)
+#endif
 
 // ---- plan ------------------------------------------------------------------------------------------------------------
 
@@ -51,13 +54,15 @@ constexpr int PACKED_UPLOAD = 120;
 struct PackedUpload {
   PackedItem item[PACKED_UPLOAD];
 };
-__global__ void pf_packed_upload_kernel(PackedUpload U, int n, PackedItem *to) {
+__global__ void pf_packed_upload_kernel(PackedUpload U, int n, PackedItem *to, int32_t *arrivals, int n_arrivals) {
   const int i = threadIdx.x;
   if (i < n) to[i] = U.item[i];
+  for (int j = i; j < n_arrivals; j += blockDim.x) arrivals[j] = 0;
 }
 
 constexpr int PACKED_WAVES = 4;
 constexpr int PACKED_ROWS = 32 * PACKED_WAVES;                    // rows of a full item
+constexpr int PACKED_ARRIVE_ROWS = 32;                            // rows that a head may have for its last workgroup to join them
 constexpr int PACKED_THIN_ROWS = 32;                              // lines of at most so many rows are thin items
 
 struct PackedParams {
@@ -68,6 +73,8 @@ struct PackedParams {
   float2 *part_ml;                                                // [planes][rows]: reference maximum, sum of weights; a sum of -1 in plane 0: the row is done
   long long q_tok, q_head, out_tok, out_head, kv_tok, kv_head, pre_tok, pre_head;    // element strides
   int n_rows, n_heads, group, block;                              // n_rows: tokens x heads
+  int32_t *arrivals;                                              // [key heads] workgroups of the head that are done; null: a second kernel joins
+  int items_per_head;
   int planes, prefix_tokens, prefix_tiles;
   unsigned group_mul, group_shift;                                // n / group = (n * group_mul) >> 32 >> group_shift
   float scale_log2;
@@ -94,7 +101,7 @@ __device__ __forceinline__ PackedParams packed_params() {
   PackedParams P = __builtin_bit_cast(PackedParams, words);
   P.q = packed_global(P.q), P.k = packed_global(P.k), P.v = packed_global(P.v), P.k_prefix = packed_global(P.k_prefix);
   P.v_prefix = packed_global(P.v_prefix), P.out = packed_global(P.out), P.items = packed_global(P.items);
-  P.part_o = packed_global(P.part_o), P.part_ml = packed_global(P.part_ml);
+  P.part_o = packed_global(P.part_o), P.part_ml = packed_global(P.part_ml), P.arrivals = packed_global(P.arrivals);
   return P;
 }
 
@@ -297,29 +304,46 @@ __device__ __forceinline__ void packed_load_q(const PackedParams &P, const Packe
 #pragma unroll
   for (int ks = 0; ks < D / 16; ++ks) qf[ks] = *(const bf16x8 *)(q + ks * 16);
 }
+// Partial results that the head's last workgroup joins cross workgroups on different dies, each with an L2 of its own: they are written and read
+// at device scope, 8 bytes at a time, past the L2; the wait for the stores before the arrival is all that stands between.
+__device__ __forceinline__ void packed_st8(void *p, float a, float b) {
+  __hip_atomic_store((unsigned long long *)p, (unsigned long long)__float_as_uint(a) | (unsigned long long)__float_as_uint(b) << 32, __ATOMIC_RELAXED,
+                     __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 packed_ld8(const void *p) {
+  const unsigned long long x = __hip_atomic_load((const unsigned long long *)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return make_float2(__uint_as_float((unsigned)x), __uint_as_float((unsigned)(x >> 32)));
+}
+
 // Where a row of an item goes: the result, or a plane's share of it.
 template <int D>
 struct PackedTo {
   __bf16 *out;
   float *part;         // null: the result
   float inv;
+  bool past_l2;
 };
 // note: this lane also notes the row's maximum and sum, and what the join has to know of the other planes
 template <int D>
 __device__ __forceinline__ PackedTo<D> packed_to(const PackedParams &P, const PackedItem &it, int row, float2 ml, bool note) {
   const int t = packed_div_group(P, row), h = packed_head(it) * P.group + row - t * P.group, plane = packed_plane(it);
   const long long id = (long long)(it.q_base + t) * P.n_heads + h;
-  PackedTo<D> to = {nullptr, nullptr, 1.0f};
+  PackedTo<D> to = {nullptr, nullptr, 1.0f, P.arrivals != nullptr};
+  auto put_ml = [&](int p, float2 x) __attribute__((always_inline)) {
+    float2 *at = P.part_ml + (long long)p * P.n_rows + id;
+    if (to.past_l2) packed_st8(at, x.x, x.y);
+    else *at = x;
+  };
   if (plane >= 0) {
     to.part = P.part_o + ((long long)plane * P.n_rows + id) * D;
     if (note) {
-      P.part_ml[(long long)plane * P.n_rows + id] = ml;
-      for (int i = 1; i <= packed_missing(it); ++i) P.part_ml[(long long)(plane + i) * P.n_rows + id] = make_float2(-3.0e38f, 0.0f);
+      put_ml(plane, ml);
+      for (int i = 1; i <= packed_missing(it); ++i) put_ml(plane + i, make_float2(-3.0e38f, 0.0f));
     }
   } else {
     to.out = P.out + (it.q_base + t) * P.out_tok + h * P.out_head;
     to.inv = ml.y > 0.0f ? 1.0f / ml.y : ml.y;                    // no key seen: zeros (a sum that is NaN stays NaN)
-    if (P.planes > 0 && note) P.part_ml[id] = make_float2(0.0f, -1.0f);
+    if (P.planes > 0 && note) put_ml(0, make_float2(0.0f, -1.0f));
   }
   return to;
 }
@@ -327,14 +351,92 @@ __device__ __forceinline__ PackedTo<D> packed_to(const PackedParams &P, const Pa
 template <int D>
 __device__ __forceinline__ void packed_put(const PackedTo<D> &to, int d0, const f32x4 &a, const f32x4 &b) {
   if (to.part) {
-    *(f32x4 *)(to.part + d0) = a;
-    *(f32x4 *)(to.part + d0 + 4) = b;
+    if (to.past_l2) {
+      packed_st8(to.part + d0, a[0], a[1]);
+      packed_st8(to.part + d0 + 2, a[2], a[3]);
+      packed_st8(to.part + d0 + 4, b[0], b[1]);
+      packed_st8(to.part + d0 + 6, b[2], b[3]);
+    } else {
+      *(f32x4 *)(to.part + d0) = a;
+      *(f32x4 *)(to.part + d0 + 4) = b;
+    }
     return;
   }
   bf16x8 w;
 #pragma unroll
   for (int i = 0; i < 4; ++i) w[i] = (__bf16)(a[i] * to.inv), w[i + 4] = (__bf16)(b[i] * to.inv);
   *(bf16x8 *)(to.out + d0) = w;
+}
+// The workgroup is done with its item.  Where there is no second kernel, the last one of its head joins the planes of the head's rows (see
+// pf_packed_join_few_kernel): D / 8 lanes take a row, four planes in flight.  Bound: the round trips to memory, one per four planes.
+template <int D>
+__device__ __forceinline__ void packed_arrive(const PackedItem &it, int32_t *s_last, int tid) {
+  const PackedParams P = packed_params();
+  if (P.arrivals == nullptr) return;
+  __builtin_amdgcn_s_waitcnt(0);                                  // this wave's partial stores have completed
+#if PF_STRICT_FENCES
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "agent");
+#endif
+  __syncthreads();
+  const int head = packed_head(it);
+  if (tid == 0) {
+#if PF_STRICT_FENCES
+    const int before = __hip_atomic_fetch_add(&P.arrivals[head], 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
+#else
+    const int before = __hip_atomic_fetch_add(&P.arrivals[head], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+#endif
+    *s_last = before == P.items_per_head - 1;
+    if (*s_last) __hip_atomic_store(&P.arrivals[head], 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);   // ready for the next launch of the plan
+  }
+  __syncthreads();
+  if (!*s_last) return;
+#if PF_STRICT_FENCES
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+#endif
+  constexpr int LANES = D / 8, AHEAD = 4;
+  const int n = P.n_rows / P.n_heads * P.group, d0 = tid % LANES * 8;
+  for (int r = tid / LANES; r < n; r += PACKED_WAVES * 64 / LANES) {
+    const int t = packed_div_group(P, r), h = head * P.group + r - t * P.group;
+    const long long id = (long long)t * P.n_heads + h;
+    float top = -3.0e38f, sum = 0.0f, acc[8] = {};
+    bool done = false;
+    for (int p0 = 0; p0 < P.planes; p0 += AHEAD) {
+      float2 ml[AHEAD], x[AHEAD][4];
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) {                           // (the last plane again once they run out)
+        const long long at = (long long)pf_min(p0 + i, P.planes - 1) * P.n_rows + id;
+        ml[i] = packed_ld8(P.part_ml + at);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[i][e] = packed_ld8(P.part_o + at * D + d0 + 2 * e);
+      }
+      if (p0 == 0 && ml[0].y == -1.0f) {                          // written by its only item
+        done = true;
+        break;
+      }
+      float new_top = top;
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) new_top = fmaxf(new_top, ml[i].x);
+      const float keep = fast_exp2((top - new_top) * P.scale_log2);
+      top = new_top;
+      sum *= keep;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[e] *= keep;
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) {
+        if (p0 + i >= P.planes || ml[i].y == 0.0f) continue;      // a plane that saw no key (or has no item) counts nothing
+        const float w = fast_exp2((ml[i].x - top) * P.scale_log2);
+        sum += w * ml[i].y;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[2 * e] += w * x[i][e].x, acc[2 * e + 1] += w * x[i][e].y;
+      }
+    }
+    if (done) continue;
+    const float inv = sum > 0.0f ? 1.0f / sum : sum;
+    bf16x8 w;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w[e] = (__bf16)(acc[e] * inv);
+    *(bf16x8 *)(P.out + t * P.out_tok + h * P.out_head + d0) = w;
+  }
 }
 // A wave's O^T (lane = row l32) as rows of LDS.
 template <int D>
@@ -449,9 +551,8 @@ __device__ __forceinline__ void packed_full(const PackedItem &it, char *smem, in
   // ---- results straight from the accumulators.  A lane holds four channels of every eight, the other half of the wave the other four: pairs
   // of quads are exchanged, after which a lane has eight channels side by side (16 bytes of the result).  Through LDS, as full rows, this
   // end of an item took 3 us instead of 1 (two barriers, and eight rounds of address arithmetic per thread). ----
-  if (!has_rows) return;
   const float lsum = partner_sum(R.l);
-  const bool valid = wrow0 + l32 < it.n_rows;
+  const bool valid = wrow0 + l32 < it.n_rows;                     // (of no lane, where the wave has no rows)
   const PackedTo<D> to = packed_to<D>(packed_params(), it, pf_min(wrow0 + l32, it.n_rows - 1), make_float2(R.m, lsum), valid && g == 0);
 #pragma unroll
   for (int db = 0; db < C::NDB; ++db)
@@ -547,6 +648,7 @@ __global__ __launch_bounds__(PACKED_WAVES * 64, 2 * 128 / D) void pf_packed_attn
   constexpr int THIN_STAGE = PACKED_WAVES * 32 * C::LD * 4;       // where a thin item joins its waves' results
   __shared__ __attribute__((aligned(1024))) char smem[2 * C::STAGE_BYTES > THIN_STAGE ? 2 * C::STAGE_BYTES : THIN_STAGE];
   __shared__ float2 s_ml[PACKED_WAVES * 32];
+  __shared__ int32_t s_last;
   // the plan was written before this launch and is constant during it: scalar loads, so that what follows from an item is scalar too
   struct Words {
     unsigned long long w[sizeof(PackedItem) / 8];
@@ -557,6 +659,7 @@ __global__ __launch_bounds__(PACKED_WAVES * 64, 2 * 128 / D) void pf_packed_attn
   const PackedItem it = __builtin_bit_cast(PackedItem, words);
   if (packed_is_thin(it)) packed_thin<D>(it, smem, s_ml, threadIdx.x);
   else packed_full<D>(it, smem, threadIdx.x);
+  packed_arrive<D>(it, &s_last, threadIdx.x);
 }
 
 // Joins the planes of every row: out = sum_p 2^((m_p - M) c) O_p / sum_p 2^((m_p - M) c) l_p.
@@ -687,6 +790,11 @@ static int packed_host_limit(const pf_packed *p, int lq, int lk, int query) {
   if (place < 0) return 0;
   return (int)std::min<long long>(lk, (place / p->block + 1) * p->block);
 }
+
+// Plan in pf_packed.work: items, then the heads' arrival counters.
+static size_t packed_plan_bytes(size_t items, int kv_heads) { return items * sizeof(PackedItem) + pf_align_up((size_t)kv_heads * sizeof(int32_t), sizeof(PackedItem)); }
+// Few rows a head: its last workgroup joins them and there is no second launch.
+static bool packed_by_arrival(const pf_packed *p) { return (long long)p->cu_q[p->n_seqs] * (p->n_heads / p->n_kv_heads) <= PACKED_ARRIVE_ROWS; }
 
 struct PackedPlan {
   std::vector<PackedItem> items;
@@ -842,7 +950,7 @@ static double packed_lay_out(const pf_packed *p, bool take_all, PackedLayout &L,
         const PackedCut cut = {whole, pf_ceil_div(most, n)};
         const int planes = planes_of(cut, &parked);
         if (planes > PACKED_MAX_PLANES || (n > 1 && (double)planes * rows * KV * (p->head_dim * 4 + 8) > 1e9)) break;
-        const double rest = planes ? C.join + parked * KV * C.plane_row : 0.0;
+        const double rest = planes ? (packed_by_arrival(p) ? 1.0 + 0.3 * planes : C.join) + parked * KV * C.plane_row : 0.0;
         if (rest >= least) break;
         // a plan with partial results has to be a good deal faster: whole launches run at their power limit, where idle places at the end
         // leave the others a higher clock
@@ -934,7 +1042,7 @@ extern "C" size_t pf_packed_work_bytes(const pf_packed *packed) {
     if (rc != PF_OK) return rc;
     PackedPlan plan;
     packed_make(packed, plan);
-    n = std::max<size_t>(1, plan.items.size()) * sizeof(PackedItem);
+    n = packed_plan_bytes(plan.items.size(), packed->n_kv_heads);
     return PF_OK;
   });
   return n;
@@ -947,14 +1055,15 @@ extern "C" int pf_packed_plan(pf_packed *packed, void *stream) {
     if (!packed->work || ((uintptr_t)packed->work & 31u)) return (int)PF_ERR_INVALID_ARG;
     PackedPlan plan;
     packed_make(packed, plan);
-    if (packed->work_bytes < std::max<size_t>(1, plan.items.size()) * sizeof(PackedItem)) return (int)PF_ERR_CAPACITY;
+    if (packed->work_bytes < packed_plan_bytes(plan.items.size(), packed->n_kv_heads)) return (int)PF_ERR_CAPACITY;
     PackedItem *to = (PackedItem *)packed->work;
     for (size_t i = 0; i < plan.items.size(); i += PACKED_UPLOAD) {
       PackedUpload U;
       const int n = (int)std::min<size_t>(PACKED_UPLOAD, plan.items.size() - i);
       memcpy(U.item, &plan.items[i], n * sizeof(PackedItem));
       if (n < PACKED_UPLOAD) memset(U.item + n, 0, (PACKED_UPLOAD - n) * sizeof(PackedItem));
-      hipLaunchKernelGGL(pf_packed_upload_kernel, dim3(1), dim3(128), 0, (hipStream_t)stream, U, n, to + i);
+      hipLaunchKernelGGL(pf_packed_upload_kernel, dim3(1), dim3(128), 0, (hipStream_t)stream, U, n, to + i, (int32_t *)(to + plan.items.size()),
+                         i == 0 ? packed->n_kv_heads : 0);
       PF_HIP_CHECK(hipGetLastError());
     }
     packed->n_items = (int32_t)plan.items.size();
@@ -980,7 +1089,7 @@ extern "C" int pf_packed_attn_fwd(const pf_packed *packed, const void *q, const 
   if (packed->n_items < 0 || packed->n_planes < 0 || packed->n_planes > PACKED_MAX_PLANES || packed->total_q != tq || packed->total_k != tk)
     return PF_ERR_INVALID_ARG;                                    // not planned, or planned for other lengths
   if (tq > 0 && packed->n_items == 0) return PF_ERR_INVALID_ARG;
-  if (!packed->work || ((uintptr_t)packed->work & 31u) || packed->work_bytes < (size_t)packed->n_items * sizeof(PackedItem)) return PF_ERR_INVALID_ARG;
+  if (!packed->work || ((uintptr_t)packed->work & 31u) || packed->work_bytes < packed_plan_bytes(packed->n_items, packed->n_kv_heads)) return PF_ERR_INVALID_ARG;
   if (!(softmax_scale >= 0.0f) || softmax_scale > 1.0e6f) return PF_ERR_INVALID_ARG;
   if (tq > 0 && (!q || !out)) return PF_ERR_INVALID_ARG;
   if (tk > 0 && (!k || !v)) return PF_ERR_INVALID_ARG;
@@ -1017,6 +1126,8 @@ extern "C" int pf_packed_attn_fwd(const pf_packed *packed, const void *q, const 
   P.planes = packed->n_planes;
   P.prefix_tokens = packed->prefix_tokens;
   P.prefix_tiles = pf_ceil_div(packed->prefix_tokens, PF_BK);
+  if (P.planes > 0 && packed_by_arrival(packed)) P.arrivals = (int32_t *)((PackedItem *)packed->work + packed->n_items);
+  P.items_per_head = packed->n_items / packed->n_kv_heads;
   P.part_o = (float *)workspace;
   P.part_ml = (float2 *)((char *)workspace + (size_t)P.planes * P.n_rows * D * 4);
   P.q_tok = q_layout ? q_layout->token_stride : D;
@@ -1034,7 +1145,7 @@ extern "C" int pf_packed_attn_fwd(const pf_packed *packed, const void *q, const 
   if (D == 128) hipLaunchKernelGGL((pf_packed_attn_kernel<128>), grid, block, 0, st, P);
   else hipLaunchKernelGGL((pf_packed_attn_kernel<64>), grid, block, 0, st, P);
   PF_HIP_CHECK(hipGetLastError());
-  if (P.planes > 0) {
+  if (P.planes > 0 && !P.arrivals) {
     const bool few = P.planes <= PACKED_FEW_PLANES;
     const dim3 rows((unsigned)pf_ceil_div(P.n_rows, few ? 256 / (D / 8) : 4));
     if (D == 128 && few) hipLaunchKernelGGL((pf_packed_join_few_kernel<128>), rows, block, 0, st, P);

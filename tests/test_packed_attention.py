@@ -313,6 +313,38 @@ def test_streams_graphs_and_two_batches_at_once():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("seqs,H,KV,P,keys", [(1, 8, 8, 0, 5000), (4, 8, 1, 3000, 70), (8, 4, 4, 700, 300), (32, 3, 3, 2000, 9), (33, 3, 3, 2000, 9)])
+def test_few_rows_split_over_many_workgroups(seqs, H, KV, P, keys, D):
+    """Up to 32 rows a head are joined by the head's last workgroup, more by a second launch: launch after launch and replay after replay
+    with the same bits, the plan's counters back at zero."""
+    cu_q, cu_k = _cu([1] * seqs), _cu([keys + 3 * i for i in range(seqs)])
+    q, k, v, kp, vp = _tensors(H, KV, D, cu_q[-1], cu_k[-1], P, 71, True)
+    want, tol = _definition(q, k, v, cu_q, cu_k, 1, kp, vp)
+    packed = B.Packed(cu_q, cu_k, H, KV, D, block=1, prefix_tokens=P, device=DEV)
+    B.pf_packed_plan(packed)
+    assert packed.c.n_planes > 1, "the case must park partial results"
+    plan = packed.work.clone()
+    ws = torch.full((B.pf_packed_workspace_bytes(packed),), 255, dtype=torch.uint8, device=DEV)
+    out = torch.full_like(q, float("nan"))
+    B.pf_packed_attn_fwd(packed, q, k, v, out, ws, kp, vp)
+    torch.cuda.synchronize()
+    assert ((out.double() - want).abs() <= tol).all()
+    graph, again = torch.cuda.CUDAGraph(), torch.empty_like(q)
+    with torch.cuda.graph(graph):
+        B.pf_packed_attn_fwd(packed, q, k, v, again, ws, kp, vp)
+    for i in range(20):
+        again.fill_(float("nan"))
+        ws.fill_(17 * i % 256)
+        if i % 2:
+            graph.replay()
+        else:
+            B.pf_packed_attn_fwd(packed, q, k, v, again, ws, kp, vp)
+        assert torch.equal(again, out)
+    assert torch.equal(packed.work, plan)
+
+
+@pytest.mark.gpu
 def test_a_prompt_taken_in_and_continued():
     """As they are used together: queries and keys of a whole prompt normalised and rotated, the prompt's attention causal by chunks, its
     keys and values taken into the ragged cache, the next chunk attended to through the cache -- and the same chunk attended to
