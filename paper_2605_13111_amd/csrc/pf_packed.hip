@@ -62,6 +62,7 @@ __global__ void pf_packed_upload_kernel(PackedUpload U, int n, PackedItem *to, i
 
 constexpr int PACKED_WAVES = 4;
 constexpr int PACKED_ROWS = 32 * PACKED_WAVES;                    // rows of a full item
+constexpr int PACKED_WIDE_ROWS = 256;                             // ... and of a wide one (pf_packed_wide.h)
 constexpr int PACKED_ARRIVE_ROWS = 32;                            // rows that a head may have for its last workgroup to join them
 constexpr int PACKED_THIN_ROWS = 32;                              // lines of at most so many rows are thin items
 
@@ -103,6 +104,18 @@ __device__ __forceinline__ PackedParams packed_params() {
   P.v_prefix = packed_global(P.v_prefix), P.out = packed_global(P.out), P.items = packed_global(P.items);
   P.part_o = packed_global(P.part_o), P.part_ml = packed_global(P.part_ml), P.arrivals = packed_global(P.arrivals);
   return P;
+}
+
+// This workgroup's item.  The plan was written before this launch and is constant during it: scalar loads, so that what follows from an item
+// is scalar too.
+__device__ __forceinline__ PackedItem packed_item() {
+  struct Words {
+    unsigned long long w[sizeof(PackedItem) / 8];
+  } words;
+  const auto *from = (const __attribute__((address_space(4))) unsigned long long *)(packed_params().items + blockIdx.x);
+#pragma unroll
+  for (int i = 0; i < (int)(sizeof(PackedItem) / 8); ++i) words.w[i] = from[i];
+  return __builtin_bit_cast(PackedItem, words);
 }
 
 template <int D>
@@ -152,7 +165,7 @@ __device__ __forceinline__ PackedKeys packed_keys(const PackedParams &P, const P
   K.v_pre = P.v_prefix + h * P.pre_head;
   return K;
 }
-// Send the copies of ROWS rows of key tile kt, from row r0 on, of K (V) into `to` (a place whose row number in its tile is a multiple of 16).
+// Send the copies of ROWS rows of key tile kt, from row r0 on (a multiple of 8), of K (V) into `to`, that row's place in the tile.
 template <int D, bool IS_V, int ROWS>
 __device__ __forceinline__ void packed_copy(const PackedParams &P, const PackedItem &it, const PackedKeys &K, int kt, int r0, char *to, int lane) {
   typedef PackedTile<D> C;
@@ -164,7 +177,7 @@ __device__ __forceinline__ void packed_copy(const PackedParams &P, const PackedI
   const unsigned rb = (unsigned)(tok * 2);                        // bytes between key rows (below 2^25: checked on the host)
   const int last = (in_prefix ? P.prefix_tokens : it.n_keys) - 1 - key0;
   const int rr = lane / C::CHUNKS, p = lane % C::CHUNKS;
-  const unsigned low = (unsigned)((p ^ (IS_V ? C::swz_v(rr) : C::swz_k(rr))) << 4);
+  const unsigned low = (unsigned)((p ^ (IS_V ? C::swz_v(rr) : C::swz_k(rr) ^ C::swz_k(r0 & 15))) << 4);
   const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void *)b, 0, -1, 0x00020000u);
   if (__builtin_expect(last >= ROWS - 1, 1)) {
     const unsigned at = (unsigned)rr * rb;
@@ -176,7 +189,7 @@ __device__ __forceinline__ void packed_copy(const PackedParams &P, const PackedI
   } else {                                                        // rows past the end repeat the last key (or, past a whole step, the one before)
     int lane_l = lane;
     asm volatile("" : "+v"(lane_l));                              // rare: its lane offsets are not held in registers through the loop
-    const unsigned low_l = (unsigned)((lane_l % C::CHUNKS ^ (IS_V ? C::swz_v(lane_l / C::CHUNKS) : C::swz_k(lane_l / C::CHUNKS))) << 4);
+    const unsigned low_l = (unsigned)((lane_l % C::CHUNKS ^ (IS_V ? C::swz_v(lane_l / C::CHUNKS) : C::swz_k(lane_l / C::CHUNKS) ^ C::swz_k(r0 & 15))) << 4);
     const __amdgpu_buffer_rsrc_t e = __builtin_amdgcn_make_buffer_rsrc((void *)(b + (long long)pf_min(last, 0) * tok), 0, -1, 0x00020000u);
     static_for<0, ROWS / C::COPY_ROWS>([&](auto gi) {
       constexpr int G = decltype(gi)::value;
@@ -369,7 +382,7 @@ __device__ __forceinline__ void packed_put(const PackedTo<D> &to, int d0, const 
 }
 // The workgroup is done with its item.  Where there is no second kernel, the last one of its head joins the planes of the head's rows (see
 // pf_packed_join_few_kernel): D / 8 lanes take a row, four planes in flight.  Bound: the round trips to memory, one per four planes.
-template <int D>
+template <int D, int WAVES>
 __device__ __forceinline__ void packed_arrive(const PackedItem &it, int32_t *s_last, int tid) {
   const PackedParams P = packed_params();
   if (P.arrivals == nullptr) return;
@@ -395,7 +408,7 @@ __device__ __forceinline__ void packed_arrive(const PackedItem &it, int32_t *s_l
 #endif
   constexpr int LANES = D / 8, AHEAD = 4;
   const int n = P.n_rows / P.n_heads * P.group, d0 = tid % LANES * 8;
-  for (int r = tid / LANES; r < n; r += PACKED_WAVES * 64 / LANES) {
+  for (int r = tid / LANES; r < n; r += WAVES * 64 / LANES) {
     const int t = packed_div_group(P, r), h = head * P.group + r - t * P.group;
     const long long id = (long long)t * P.n_heads + h;
     float top = -3.0e38f, sum = 0.0f, acc[8] = {};
@@ -446,6 +459,30 @@ __device__ __forceinline__ void packed_stage(float *row, const f32x16 (&o)[D / 3
 #pragma unroll
     for (int i4 = 0; i4 < 4; ++i4)
       *(f32x4 *)(row + db * 32 + 8 * i4 + 4 * g) = f32x4{o[db][i4 * 4], o[db][i4 * 4 + 1], o[db][i4 * 4 + 2], o[db][i4 * 4 + 3]};
+}
+
+// A wave's results straight from the accumulators.  A lane holds four channels of every eight, the other half of the wave the other four: pairs
+// of quads are exchanged, after which a lane has eight channels side by side (16 bytes of the result).  Through LDS, as full rows, this
+// end of an item took 3 us instead of 1 (two barriers, and eight rounds of address arithmetic per thread).
+template <int D>
+__device__ __forceinline__ void packed_results(const PackedItem &it, int wrow0, const f32x16 (&o)[D / 32], const PackedRow &R, int lane) {
+  const int l32 = lane & 31, g = lane >> 5;
+  const float lsum = partner_sum(R.l);
+  const bool valid = wrow0 + l32 < it.n_rows;                     // (of no lane, where the wave has no rows)
+  const PackedTo<D> to = packed_to<D>(packed_params(), it, pf_min(wrow0 + l32, it.n_rows - 1), make_float2(R.m, lsum), valid && g == 0);
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int pair = 0; pair < 2; ++pair) {
+      f32x4 x, y;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_int(o[db][pair * 8 + i]), __float_as_int(o[db][pair * 8 + 4 + i]), false, false);
+        x[i] = __int_as_float(r[0]);
+        y[i] = __int_as_float(r[1]);
+      }
+      if (valid) packed_put<D>(to, db * 32 + (2 * pair + g) * 8, x, y);
+    }
 }
 
 // ---- a full item: 128 rows, 32 a wave; the waves share every key tile, two stages of tiles copied global -> LDS directly ----
@@ -548,25 +585,7 @@ __device__ __forceinline__ void packed_full(const PackedItem &it, char *smem, in
     packed_softmax<D, 2>(s, pf, o, R, c);
     packed_pv<D, 4>(o, pf, av + stage);
   }
-  // ---- results straight from the accumulators.  A lane holds four channels of every eight, the other half of the wave the other four: pairs
-  // of quads are exchanged, after which a lane has eight channels side by side (16 bytes of the result).  Through LDS, as full rows, this
-  // end of an item took 3 us instead of 1 (two barriers, and eight rounds of address arithmetic per thread). ----
-  const float lsum = partner_sum(R.l);
-  const bool valid = wrow0 + l32 < it.n_rows;                     // (of no lane, where the wave has no rows)
-  const PackedTo<D> to = packed_to<D>(packed_params(), it, pf_min(wrow0 + l32, it.n_rows - 1), make_float2(R.m, lsum), valid && g == 0);
-#pragma unroll
-  for (int db = 0; db < C::NDB; ++db)
-#pragma unroll
-    for (int pair = 0; pair < 2; ++pair) {
-      f32x4 x, y;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_int(o[db][pair * 8 + i]), __float_as_int(o[db][pair * 8 + 4 + i]), false, false);
-        x[i] = __int_as_float(r[0]);
-        y[i] = __int_as_float(r[1]);
-      }
-      if (valid) packed_put<D>(to, db * 32 + (2 * pair + g) * 8, x, y);
-    }
+  packed_results<D>(it, wrow0, o, R, lane);
 }
 
 // ---- a thin item: 32 rows that all waves hold, the keys split over the waves.  Each streams steps of 32 keys through a place of its own in
@@ -649,18 +668,14 @@ __global__ __launch_bounds__(PACKED_WAVES * 64, 2 * 128 / D) void pf_packed_attn
   __shared__ __attribute__((aligned(1024))) char smem[2 * C::STAGE_BYTES > THIN_STAGE ? 2 * C::STAGE_BYTES : THIN_STAGE];
   __shared__ float2 s_ml[PACKED_WAVES * 32];
   __shared__ int32_t s_last;
-  // the plan was written before this launch and is constant during it: scalar loads, so that what follows from an item is scalar too
-  struct Words {
-    unsigned long long w[sizeof(PackedItem) / 8];
-  } words;
-  const auto *from = (const __attribute__((address_space(4))) unsigned long long *)(packed_params().items + blockIdx.x);
-#pragma unroll
-  for (int i = 0; i < (int)(sizeof(PackedItem) / 8); ++i) words.w[i] = from[i];
-  const PackedItem it = __builtin_bit_cast(PackedItem, words);
+  const PackedItem it = packed_item();
   if (packed_is_thin(it)) packed_thin<D>(it, smem, s_ml, threadIdx.x);
   else packed_full<D>(it, smem, threadIdx.x);
-  packed_arrive<D>(it, &s_last, threadIdx.x);
+  packed_arrive<D, PACKED_WAVES>(it, &s_last, threadIdx.x);
 }
+
+#include "pf_packed_wide.h"
+
 
 // Joins the planes of every row: out = sum_p 2^((m_p - M) c) O_p / sum_p 2^((m_p - M) c) l_p.
 //
@@ -799,6 +814,7 @@ static bool packed_by_arrival(const pf_packed *p) { return (long long)p->cu_q[p-
 struct PackedPlan {
   std::vector<PackedItem> items;
   int planes = 0;
+  bool wide = false;           // items of 256 rows (head_dim 128)
 };
 
 // Rows that share their keys: one sequence's, or in front of the prefix those of neighbouring sequences.
@@ -806,7 +822,7 @@ struct PackedLine {
   int q_base, n_rows, k_base, n_keys;
   bool prefix;                 // has the prefix's tiles
   int stack;                   // >= 0: the line that has the prefix in this one's place; -1: this line has all of its rows' keys; -2: it is such a line
-  bool thin() const { return n_rows <= PACKED_THIN_ROWS; }
+  bool thin;                   // goes by thin items
 };
 struct PackedRowTile {
   int line, row0, n_kt;
@@ -818,16 +834,17 @@ struct PackedRowTile {
 // places taken: a full item's key tile, and a key tile that no other row tile reads from memory; few taken: a key tile of a full and of a thin item.
 // An item's set-up and end; the second launch; a row of a plane written and read.
 struct PackedCosts {
-  int places;
+  int rows, thin_rows, places; // of a full item; of a thin one at most; workgroups on the chip at once
   double tile, tile_alone, tile_few, tile_thin, item, join, plane_row;
 };
-static PackedCosts packed_costs(int head_dim) {
-  if (head_dim == 128) return {512, 1.95, 3.4, 1.15, 0.42, 3.0, 6.0, 2.3e-4};
-  return {1024, 2.3, 3.4, 0.85, 0.32, 3.0, 6.0, 1.2e-4};
+static PackedCosts packed_costs(int head_dim, bool wide) {
+  if (wide) return {PACKED_WIDE_ROWS, 0, 256, 1.8, 1.8, 1.5, 0.35, 5.0, 6.0, 2.3e-4};
+  if (head_dim == 128) return {PACKED_ROWS, PACKED_THIN_ROWS, 512, 1.95, 3.4, 1.15, 0.42, 3.0, 6.0, 2.3e-4};
+  return {PACKED_ROWS, PACKED_THIN_ROWS, 1024, 2.3, 3.4, 0.85, 0.32, 3.0, 6.0, 1.2e-4};
 }
 
-static int packed_line_tiles(const pf_packed *p, const PackedLine &l, int row0, int pre_kt) {
-  const int G = p->n_heads / p->n_kv_heads, last = pf_min(row0 + PACKED_ROWS, l.n_rows) - 1;
+static int packed_line_tiles(const pf_packed *p, const PackedLine &l, int row0, int rows, int pre_kt) {
+  const int G = p->n_heads / p->n_kv_heads, last = pf_min(row0 + rows, l.n_rows) - 1;
   const int own = l.n_keys > 0 ? pf_ceil_div(packed_host_limit(p, l.n_rows / G, l.n_keys, last / G), PF_BK) : 0;
   return own + (l.prefix ? pre_kt : 0);
 }
@@ -877,12 +894,12 @@ static double packed_time(const std::vector<PackedRowTile> &tiles, int heads, co
 struct PackedLayout {
   std::vector<PackedLine> lines;
   std::vector<PackedRowTile> tiles;
+  std::vector<int> cuts, first;  // of every row tile: into how many items its keys are cut, the plane of the first
   int planes = 0;
 };
-static double packed_lay_out(const pf_packed *p, bool take_all, PackedLayout &L, std::vector<int> &cuts, std::vector<int> &first) {
-  const int G = p->n_heads / p->n_kv_heads, KV = p->n_kv_heads, BQ = PACKED_ROWS;
+static double packed_lay_out(const pf_packed *p, const PackedCosts &C, bool take_all, PackedLayout &L) {
+  const int G = p->n_heads / p->n_kv_heads, KV = p->n_kv_heads, BQ = C.rows;
   const int pre_kt = pf_ceil_div(p->prefix_tokens, PF_BK);
-  const PackedCosts C = packed_costs(p->head_dim);
   std::vector<PackedLine> &lines = L.lines;
   std::vector<PackedRowTile> &tiles = L.tiles;
   int stack = -1;
@@ -891,33 +908,34 @@ static double packed_lay_out(const pf_packed *p, bool take_all, PackedLayout &L,
     const int lq = p->cu_q[s + 1] - p->cu_q[s], r = lq * G;
     if (lq == 0) continue;
     // the rows that its tiles would leave empty in front of the prefix, against parking its rows' partial results
-    const double empty = r <= PACKED_THIN_ROWS ? 1.0 : pf_ceil_div(r, BQ) - (double)r / BQ;
+    const double empty = r <= C.thin_rows ? 1.0 : pf_ceil_div(r, BQ) - (double)r / BQ;
     const bool own = pre_kt == 0 || take_all || empty * pre_kt * C.tile / C.places < 2.0 * r * C.plane_row;
     if (own) {
       stack = -1;
     } else {
       if (stack < 0) {
         stack = (int)lines.size();
-        lines.push_back({p->cu_q[s], 0, 0, 0, true, -2});
+        lines.push_back({p->cu_q[s], 0, 0, 0, true, -2, false});
       }
       lines[stack].n_rows += r;
       any_stack = true;
     }
-    lines.push_back({p->cu_q[s], r, p->cu_k[s], p->cu_k[s + 1] - p->cu_k[s], pre_kt > 0 && own, stack});
+    lines.push_back({p->cu_q[s], r, p->cu_k[s], p->cu_k[s + 1] - p->cu_k[s], pre_kt > 0 && own, stack, false});
   }
+  for (PackedLine &l : lines) l.thin = l.n_rows <= C.thin_rows;
   long long rows = 0, with_prefix = 0;
   for (const PackedLine &l : lines)
     if (l.prefix) with_prefix += pf_ceil_div(l.n_rows, BQ);
   // a key tile's time in full tiles: what its bytes take where row tiles that read them are few, if that is more
   auto load_of = [&](int n_pre, int n_own, const PackedLine &l) {
-    const double least = l.thin() ? C.tile_thin / C.tile_few : 1.0, alone = C.tile_alone / C.tile;
+    const double least = l.thin ? C.tile_thin / C.tile_few : 1.0, alone = C.tile_alone / C.tile;
     const double pre = std::max(least, alone / std::max(1ll, with_prefix)), own = std::max(least, alone / pf_ceil_div(l.n_rows, BQ));
     return (int)ceil(n_pre * pre + n_own * own - 1e-9);
   };
   for (size_t l = 0; l < lines.size(); ++l)
     for (int r0 = 0; r0 < lines[l].n_rows; r0 += BQ) {
-      const int n_kt = packed_line_tiles(p, lines[l], r0, pre_kt), pre = lines[l].prefix ? pre_kt : 0;
-      tiles.push_back({(int)l, r0, n_kt, lines[l].thin(), load_of(pre, n_kt - pre, lines[l])});
+      const int n_kt = packed_line_tiles(p, lines[l], r0, BQ, pre_kt), pre = lines[l].prefix ? pre_kt : 0;
+      tiles.push_back({(int)l, r0, n_kt, lines[l].thin, load_of(pre, n_kt - pre, lines[l])});
       if (lines[l].stack != -2) rows += pf_min(BQ, lines[l].n_rows - r0);
     }
   std::stable_sort(tiles.begin(), tiles.end(), [](const PackedRowTile &a, const PackedRowTile &b) { return a.load > b.load; });
@@ -970,21 +988,25 @@ static double packed_lay_out(const pf_packed *p, bool take_all, PackedLayout &L,
   L.planes = planes_of(best, &parked);
   for (size_t i = 0; i < tiles.size(); ++i) {
     const int st = lines[tiles[i].line].stack;
-    cuts.push_back(cuts_of(best, i));
-    first.push_back(st >= 0 ? stack_cuts(st, best.seg) : 0);
+    L.cuts.push_back(cuts_of(best, i));
+    L.first.push_back(st >= 0 ? stack_cuts(st, best.seg) : 0);
   }
   return least;
 }
 
 static void packed_make(const pf_packed *p, PackedPlan &plan) {
-  PackedLayout L, all;
-  std::vector<int> cuts, first, cuts_all, first_all;
-  double t = packed_lay_out(p, false, L, cuts, first);
-  if (L.planes > 0 && p->prefix_tokens > 0 && packed_lay_out(p, true, all, cuts_all, first_all) < t) {
-    L = std::move(all);
-    cuts.swap(cuts_all);
-    first.swap(first_all);
-  }
+  PackedLayout L;
+  double least = 1e300;
+  for (int wide = 0; wide < (p->head_dim == 128 ? 2 : 1); ++wide)
+    for (int take_all = 0; take_all < (p->prefix_tokens > 0 ? 2 : 1); ++take_all) {
+      PackedLayout other;
+      const double t = packed_lay_out(p, packed_costs(p->head_dim, wide != 0), take_all != 0, other);
+      if (t < least) {
+        least = t;
+        L = std::move(other);
+        plan.wide = wide != 0;
+      }
+    }
   plan.planes = L.planes;
   struct Loaded {
     PackedItem item;
@@ -995,14 +1017,14 @@ static void packed_make(const pf_packed *p, PackedPlan &plan) {
     for (size_t t = 0; t < L.tiles.size(); ++t) {
       const PackedRowTile &tile = L.tiles[t];
       const PackedLine &l = L.lines[tile.line];
-      const int n = cuts[t];
+      const int n = L.cuts[t];
       for (int i = 0; i < n; ++i) {
         PackedItem it = {l.q_base, tile.row0, l.n_rows, l.k_base, l.n_keys, pf_seg_begin(tile.n_kt, n, i), pf_seg_begin(tile.n_kt, n, i + 1), h};
         if (l.prefix) it.head |= 1 << PACKED_PREFIX_BIT;
         if (tile.thin) it.head |= (int)(1u << 31);
         if (!(l.stack == -1 && n == 1)) {
-          it.head |= (first[t] + i + 1) << 13;
-          if (i == n - 1 && l.stack != -2) it.head |= (L.planes - first[t] - n) << 22;
+          it.head |= (L.first[t] + i + 1) << 13;
+          if (i == n - 1 && l.stack != -2) it.head |= (L.planes - L.first[t] - n) << 22;
         }
         items.push_back({it, tile.load / n});
       }
@@ -1068,6 +1090,7 @@ extern "C" int pf_packed_plan(pf_packed *packed, void *stream) {
     }
     packed->n_items = (int32_t)plan.items.size();
     packed->n_planes = plan.planes;
+    packed->kernel = plan.wide ? 1 : 0;
     packed->total_q = packed->cu_q[packed->n_seqs];
     packed->total_k = packed->cu_k[packed->n_seqs];
     return (int)PF_OK;
@@ -1086,7 +1109,7 @@ extern "C" int pf_packed_attn_fwd(const pf_packed *packed, const void *q, const 
   const int rc = packed_check(packed);
   if (rc != PF_OK) return rc;
   const int tq = packed->cu_q[packed->n_seqs], tk = packed->cu_k[packed->n_seqs], D = packed->head_dim;
-  if (packed->n_items < 0 || packed->n_planes < 0 || packed->n_planes > PACKED_MAX_PLANES || packed->total_q != tq || packed->total_k != tk)
+  if (packed->n_items < 0 || packed->kernel < 0 || packed->kernel > (D == 128 ? 1 : 0) || packed->n_planes < 0 || packed->n_planes > PACKED_MAX_PLANES || packed->total_q != tq || packed->total_k != tk)
     return PF_ERR_INVALID_ARG;                                    // not planned, or planned for other lengths
   if (tq > 0 && packed->n_items == 0) return PF_ERR_INVALID_ARG;
   if (!packed->work || ((uintptr_t)packed->work & 31u) || packed->work_bytes < packed_plan_bytes(packed->n_items, packed->n_kv_heads)) return PF_ERR_INVALID_ARG;
@@ -1142,7 +1165,8 @@ extern "C" int pf_packed_attn_fwd(const pf_packed *packed, const void *q, const 
   P.scale_log2 = scale * 1.4426950408889634f;
   hipStream_t st = (hipStream_t)stream;
   const dim3 grid(packed->n_items), block(PACKED_WAVES * 64);
-  if (D == 128) hipLaunchKernelGGL((pf_packed_attn_kernel<128>), grid, block, 0, st, P);
+  if (packed->kernel == 1) hipLaunchKernelGGL(pf_packed_wide_kernel, grid, dim3(WIDE_WAVES * 64), 0, st, P);
+  else if (D == 128) hipLaunchKernelGGL((pf_packed_attn_kernel<128>), grid, block, 0, st, P);
   else hipLaunchKernelGGL((pf_packed_attn_kernel<64>), grid, block, 0, st, P);
   PF_HIP_CHECK(hipGetLastError());
   if (P.planes > 0 && !P.arrivals) {

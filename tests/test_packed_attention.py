@@ -197,6 +197,24 @@ def test_longer_sequences(H, KV, D, block, P):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("lq,lk,P,block", [
+    ([1300, 513, 257, 1], None, 0, 1), ([1300, 513, 257, 1], None, 1500, 1), ([1000, 700], None, 0, 300), ([64, 900, 0, 255], [64, 2900, 70, 255], 0, 1),
+    ([900, 900], [200, 700], 0, 1), ([901], [901], 130, 0), ([129, 300, 40], [1000, 1000, 1000], 64, 48), ([1200], [1200], 0, 2 ** 31 - 1)])
+def test_launches_of_wide_items(lq, lk, P, block):
+    """Enough work for items of 256 rows (head_dim 128): rows that end inside an item, rows that see nothing, a wave of a tile each with an end
+    of its own, prefixes that end inside a tile."""
+    lk = lq if lk is None else lk
+    D = 128
+    for KV, G in [(n, g) for g in (2, 5, 1) for n in range(8, 65, 4)]:   # the first numbers of heads that the planner takes wide items for
+        packed = B.Packed(_cu(lq), _cu(lk), KV * G, KV, D, block=block, prefix_tokens=P, device=DEV)
+        B.pf_packed_plan(packed)
+        if packed.c.kernel == 1:
+            break
+    assert packed.c.kernel == 1, "the case must go by wide items"
+    _case(_cu(lq), _cu(lk), KV * G, KV, D, block, P, seed=17)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("seqs,P,H,KV", [(1, 0, 8, 1), (1, 9000, 4, 4), (40, 3333, 8, 2), (150, 129, 2, 2)])
 def test_single_tokens_of_many_sequences(D, seqs, P, H, KV):
