@@ -153,6 +153,9 @@ def _check(status, what):
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
 
 
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
 def _stream(stream):
     return _raw_stream(torch.cuda.current_device()) if stream is None else stream
 
@@ -385,7 +388,7 @@ _NO_ROWS = bytes(_ROWS.size)
 assert _ROWS.size == ctypes.sizeof(pf_rope_rows) and _LAYOUT.size == ctypes.sizeof(pf_chunk_layout)
 
 
-def _rope_rows(D, n_tokens, x, out, weight):
+def _rope_rows(D, n_tokens, dev, x, out, weight):
     """A tensor and its result as a ``pf_rope_rows`` struct: bf16 views of logical shape [heads, tokens, head_dim]."""
     if x is None:
         assert out is None and weight is None
@@ -395,22 +398,27 @@ def _rope_rows(D, n_tokens, x, out, weight):
     xh, xt, x1 = x.stride()
     oh, ot, o1 = out.stride()
     assert x.dtype is _BF16 and out.dtype is _BF16 and out.shape == shape and tokens == n_tokens and d == D and x1 == 1 and o1 == 1
-    if weight is None:
-        return _ROWS.pack(x.data_ptr(), out.data_ptr(), 0, heads, 0, xt, xh, ot, oh)
-    assert weight.dtype is _BF16 and weight.shape == (D,) and weight.is_contiguous()
-    return _ROWS.pack(x.data_ptr(), out.data_ptr(), weight.data_ptr(), heads, 0, xt, xh, ot, oh)
+    assert x.get_device() == dev and out.get_device() == dev
+    w = 0
+    if weight is not None:
+        assert weight.dtype is _BF16 and weight.shape == (D,) and weight.stride(0) == 1 and weight.get_device() == dev
+        w = weight.data_ptr()
+    return _ROWS.pack(x.data_ptr(), out.data_ptr(), w, heads, 0, xt, xh, ot, oh)
 
 
 def pf_qk_norm_rope(rope, positions, q, q_out, k=None, k_out=None, q_weight=None, k_weight=None, eps=0.0, stream=None):
     """RMS norm per head (eps > 0) and rotation of queries and keys in one launch.  q, k, q_out, k_out: bf16 views of logical shape [heads,
     tokens, head_dim], e.g. [tokens, heads, head_dim] tensors seen heads first; q_out may be q.  Either pair may be None.  positions: int32
-    [axes, tokens], contiguous."""
-    n_tokens = (k if q is None else q).shape[1]
+    [axes, tokens], contiguous.  All on the current device."""
+    n_tokens, dev, D = (k if q is None else q).shape[1], _current_device(), rope.head_dim
+    at = 0
     if rope.rot_dim:
-        assert positions.dtype is torch.int32 and positions.is_contiguous() and positions.shape == (rope.n_axes, n_tokens)
-    D = rope.head_dim
-    _check(lib().pf_qk_norm_rope(ctypes.byref(rope), n_tokens, _ptr(positions), _rope_rows(D, n_tokens, q, q_out, q_weight),
-                                 _rope_rows(D, n_tokens, k, k_out, k_weight), eps, _stream(stream)), "pf_qk_norm_rope")
+        assert positions.dtype is torch.int32 and positions.is_contiguous() and positions.shape == (rope.n_axes, n_tokens) and positions.get_device() == dev
+        at = positions.data_ptr()
+    rc = (_lib or lib()).pf_qk_norm_rope(ctypes.byref(rope), n_tokens, at, _rope_rows(D, n_tokens, dev, q, q_out, q_weight),
+                                         _rope_rows(D, n_tokens, dev, k, k_out, k_weight), eps, _raw_stream(dev) if stream is None else stream)
+    if rc:
+        raise PfError(rc, "pf_qk_norm_rope")
 
 
 class Packed:
@@ -435,6 +443,7 @@ class Packed:
 
 
 def pf_packed_plan(packed, stream=None):
+    assert packed.work.get_device() == _current_device()
     _check(lib().pf_packed_plan(ctypes.byref(packed.c), _stream(stream)), "pf_packed_plan")
 
 
@@ -442,27 +451,33 @@ def pf_packed_workspace_bytes(packed):
     return int(lib().pf_packed_workspace_bytes(ctypes.byref(packed.c)))
 
 
-def _packed_layout(heads, tokens, D, a, b=None):
+def _packed_layout(heads, tokens, D, dev, a, b=None):
     """Checks of a tensor, or of two that share a layout; the layout.  They may hold more tokens than the batch has."""
     shape, stride = a.shape, a.stride()
-    assert shape[0] == heads and shape[1] >= tokens and shape[2] == D and stride[2] == 1 and a.dtype is _BF16
-    assert b is None or (b.dtype is _BF16 and b.shape == shape and b.stride() == stride)
+    assert shape[0] == heads and shape[1] >= tokens and shape[2] == D and stride[2] == 1 and a.dtype is _BF16 and a.get_device() == dev
+    assert b is None or (b.dtype is _BF16 and b.shape == shape and b.stride() == stride and b.get_device() == dev)
     return _LAYOUT.pack(stride[1], stride[0])
 
 
 def pf_packed_attn_fwd(packed, q, k, v, out, workspace, k_prefix=None, v_prefix=None, softmax_scale=0.0, stream=None):
     """q, out: bf16 views of logical shape [n_heads, total_q, head_dim]; k, v: [n_kv_heads, total_k, head_dim]; k_prefix, v_prefix:
     [n_kv_heads, prefix_tokens, head_dim] -- e.g. [tokens, heads, head_dim] tensors seen heads first; no copy is made.  k and v share a
-    stride pattern, and so do the prefix's.  workspace: uint8 tensor."""
-    H, KV, tq, D = packed.n_heads, packed.n_kv_heads, packed.total_q, packed.D
+    stride pattern, and so do the prefix's.  workspace: uint8 tensor.  All on the current device, which is the plan's."""
+    H, KV, tq, D, dev = packed.n_heads, packed.n_kv_heads, packed.total_q, packed.D, _current_device()
     kp = vp = pl = None
     if packed.prefix_tokens:
-        pl = _packed_layout(KV, packed.prefix_tokens, D, k_prefix, v_prefix)
+        pl = _packed_layout(KV, packed.prefix_tokens, D, dev, k_prefix, v_prefix)
         kp, vp = k_prefix.data_ptr(), v_prefix.data_ptr()
-    _check(lib().pf_packed_attn_fwd(ctypes.byref(packed.c), q.data_ptr(), _packed_layout(H, tq, D, q), k.data_ptr(), v.data_ptr(),
-                                    _packed_layout(KV, packed.total_k, D, k, v), kp, vp, pl, out.data_ptr(), _packed_layout(H, tq, D, out),
-                                    softmax_scale, _ptr(workspace), 0 if workspace is None else workspace.nbytes, _stream(stream)),
-           "pf_packed_attn_fwd")
+    ws = ws_bytes = 0
+    if workspace is not None:
+        assert workspace.get_device() == dev and workspace.is_contiguous()
+        ws, ws_bytes = workspace.data_ptr(), workspace.nbytes
+    assert packed.work.get_device() == dev
+    rc = (_lib or lib()).pf_packed_attn_fwd(ctypes.byref(packed.c), q.data_ptr(), _packed_layout(H, tq, D, dev, q), k.data_ptr(), v.data_ptr(),
+                                            _packed_layout(KV, packed.total_k, D, dev, k, v), kp, vp, pl, out.data_ptr(),
+                                            _packed_layout(H, tq, D, dev, out), softmax_scale, ws, ws_bytes, _raw_stream(dev) if stream is None else stream)
+    if rc:
+        raise PfError(rc, "pf_packed_attn_fwd")
 
 
 def pf_classify_heads(logits, alpha=0.8, beta=6.4, with_periods=True, stream=None):

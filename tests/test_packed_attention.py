@@ -98,6 +98,12 @@ def test_calls_refused_without_a_device():
     assert call(s, kp=fake, vp=fake, pl=(128, 128), ws=0x20000, ws_bytes=need) == bad
 
 
+def test_tensors_of_another_device_are_refused():
+    """Host memory instead of device memory never reaches a kernel."""
+    with pytest.raises((AssertionError, RuntimeError)):
+        B.pf_packed_plan(B.Packed([0, 4], [0, 4], 2, 2, 64, device="cpu"))
+
+
 # ---- results ----------------------------------------------------------------------------------------------------------
 
 def _definition(q, k, v, cu_q, cu_k, block, kp=None, vp=None, scale=None):
@@ -228,6 +234,21 @@ def test_single_tokens_of_many_sequences(D, seqs, P, H, KV):
 def test_sharp_and_flat_softmax(gain, scale, D):
     """Scores far apart: the reference maximum moves many times; masked tiles in front of it."""
     _case(_cu([100, 300]), _cu([100, 300]), 4, 2, D, 1, 90, seed=7, gain=gain, scale=scale)
+
+
+@pytest.mark.gpu
+def test_host_tensors_are_refused():
+    cu = [0, 7]
+    q, k, v, kp, vp = _tensors(2, 2, 64, 7, 7, 5, 1, True)
+    packed = B.Packed(cu, cu, 2, 2, 64, prefix_tokens=5, device=DEV)
+    B.pf_packed_plan(packed)
+    ws = torch.empty(B.pf_packed_workspace_bytes(packed), dtype=torch.uint8, device=DEV)
+    good = [q, k, v, torch.empty_like(q), ws, kp, vp]
+    B.pf_packed_attn_fwd(packed, *good)
+    for i in range(7):
+        with pytest.raises(AssertionError):
+            B.pf_packed_attn_fwd(packed, *(t.cpu() if j == i else t for j, t in enumerate(good)))
+    torch.cuda.synchronize()
 
 
 @pytest.mark.gpu

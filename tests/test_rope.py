@@ -201,6 +201,18 @@ def test_in_place_equals_out_of_place_and_the_rest_of_the_buffer_stays():
 
 
 @pytest.mark.gpu
+def test_host_tensors_are_refused():
+    rope, pos = B.make_rope(64), torch.zeros((1, 3), dtype=torch.int32, device=DEV)
+    q, w = synth.randn_bf16((2, 3, 64), 1, device=DEV), synth.randn_bf16((64,), 2, device=DEV)
+    good = [pos, q, q.clone(), q.clone(), q.clone(), w, w]
+    B.pf_qk_norm_rope(rope, *good, eps=1e-6)
+    for i in range(7):
+        with pytest.raises(AssertionError):
+            B.pf_qk_norm_rope(rope, *(t.cpu() if j == i else t for j, t in enumerate(good)), eps=1e-6)
+    torch.cuda.synchronize()
+
+
+@pytest.mark.gpu
 def test_zero_rows_and_rows_that_are_not_finite():
     """A row of zeros stays zero; a NaN or an infinity stays in its own row."""
     D = 64
