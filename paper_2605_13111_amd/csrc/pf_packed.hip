@@ -874,15 +874,20 @@ static double packed_time(const std::vector<PackedRowTile> &tiles, int heads, co
     const int cuts = cut.of((int)i, tiles[i]);
     count[pf_ceil_div(tiles[i].load, cuts)] += cuts * heads;      // (a run may be a tile shorter)
   }
-  // heaviest first, each to the place that is free first
-  std::priority_queue<double, std::vector<double>, std::greater<double>> free_at;
-  for (int i = 0; i < C.places; ++i) free_at.push(0.0);
+  // heaviest first, each to the place that is free first; places that become free together go on together
+  typedef std::pair<double, int> Free;
+  std::priority_queue<Free, std::vector<Free>, std::greater<Free>> free_at;
+  free_at.push({0.0, C.places});
   double end = C.item + few;
   for (int t = longest; t >= 0; --t)
-    for (int i = 0; i < count[t]; ++i) {
-      const double at = free_at.top() + C.item + t * C.tile;
+    for (int left = count[t]; left > 0;) {
+      const Free first = free_at.top();
+      const int n_taken = std::min(left, first.second);
+      const double at = first.first + C.item + t * C.tile;
       free_at.pop();
-      free_at.push(at);
+      if (first.second > n_taken) free_at.push({first.first, first.second - n_taken});
+      free_at.push({at, n_taken});
+      left -= n_taken;
       end = std::max(end, at);
       if (end > limit) return 1e300;
     }
@@ -972,7 +977,8 @@ static double packed_lay_out(const pf_packed *p, const PackedCosts &C, bool take
         if (rest >= least) break;
         // a plan with partial results has to be a good deal faster: whole launches run at their power limit, where idle places at the end
         // leave the others a higher clock
-        const double t = (packed_time(tiles, KV, cut, C, least) + rest) * (planes && !any_stack ? 1.1 : 1.0);
+        const double handicap = planes && !any_stack ? 1.1 : 1.0;
+        const double t = (packed_time(tiles, KV, cut, C, least / handicap - rest) + rest) * handicap;
         if (t < least) {
           least = t;
           best = cut;
