@@ -357,7 +357,7 @@ typedef struct pf_rope_rows {
  * and pf_cache_append_strided take.
  *   positions  dev int32 [n_axes][n_tokens], any values; may be NULL when rot_dim is 0
  *   eps        > 0; 0 = no norm (weights must be NULL then)
- * q and k must not be NULL; one of them may have n_heads = 0.  n_tokens = 0 does nothing.
+ * q and k must not be NULL; one of them may have n_heads = 0.  n_tokens = 0 does nothing; at most 2^26 - 1.
  */
 int pf_qk_norm_rope(const pf_rope *rope, int n_tokens, const int32_t *positions, const pf_rope_rows *q,
                     const pf_rope_rows *k, float eps, void *stream);
@@ -385,19 +385,21 @@ typedef struct pf_packed {
   /* [lib] written by pf_packed_plan */
   int32_t n_items, n_planes;      /* work items; partial results that a row may have */
   int32_t total_q, total_k;       /* tokens planned for */
-  int32_t kernel;
+  int32_t kernel;                 /* kind of items */
   const int32_t *cu_q;            /* host [n_seqs+1], cu_q[0] = 0, not decreasing */
   const int32_t *cu_k;            /* host [n_seqs+1], cu_k[0] = 0, not decreasing */
   void *work;                     /* dev, >= pf_packed_work_bytes, 32-byte aligned */
   size_t work_bytes;
+  uint64_t planned_for;           /* [lib] checksum of the lengths, heads, block and prefix that the plan is for, and of the plan's own sizes */
 } pf_packed;
 
 /* Bytes of pf_packed.work that pf_packed_plan needs for these lengths; 0 on a bad argument.  Host only. */
 size_t pf_packed_work_bytes(const pf_packed *packed);
 
 /* Plan the batch: what pf_packed_attn_fwd does for these lengths, heads and block, for any number of calls (the layers of a
- * model).  Writes `work` on the stream (captured into a graph, a replay writes the same plan again).
- * PF_ERR_CAPACITY if work_bytes is too small. */
+ * model).  Writes `work` on the stream (captured into a graph, a replay writes the same plan again).  A change of lengths, heads,
+ * head_dim, block or prefix needs a plan of its own: until then the calls below refuse the batch.
+ * PF_ERR_CAPACITY if work_bytes is too small; PF_ERR_UNSUPPORTED if the batch is more than 2^23 - 1 work items. */
 int pf_packed_plan(pf_packed *packed, void *stream);
 
 /* Bytes of workspace that pf_packed_attn_fwd needs under the plan (partial results of rows whose keys are split); 0 on a bad
@@ -412,12 +414,12 @@ size_t pf_packed_workspace_bytes(const pf_packed *packed);
  * every key that a sequence owns.
  *   q, out              dev [n_heads][total_q][head_dim] or by q_layout and out_layout
  *   k, v                dev [n_kv_heads][total_k][head_dim] or by kv_layout
- *   k_prefix, v_prefix  dev [n_kv_heads][prefix_tokens][head_dim] or by prefix_layout; NULL without a prefix
+ *   k_prefix, v_prefix  dev [n_kv_heads][prefix_tokens][head_dim] or by prefix_layout; must be NULL without a prefix
  *   softmax_scale       0 = 1/sqrt(head_dim)
  *   workspace           dev, >= pf_packed_workspace_bytes, 16-byte aligned
- * 16-byte aligned tensors; a NULL layout = packed per head.  The plan (it holds arrival counters) and the workspace are
- * written by the launch and left ready for the next one: launches that share either must not overlap in time (same
- * stream, or ordered by events).
+ * 16-byte aligned tensors; a NULL layout = packed per head.  out must not overlap any other tensor.  The plan (it holds arrival
+ * counters) and the workspace are written by the launch and left ready for the next one: launches that share either, and
+ * pf_packed_plan on the same `work`, must not overlap in time (same stream, or ordered by events).
  */
 int pf_packed_attn_fwd(const pf_packed *packed, const void *q, const pf_chunk_layout *q_layout, const void *k, const void *v,
                        const pf_chunk_layout *kv_layout, const void *k_prefix, const void *v_prefix,

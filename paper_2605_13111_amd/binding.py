@@ -71,7 +71,8 @@ class pf_rope_rows(ctypes.Structure):
 class pf_packed(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("n_seqs", "n_heads", "n_kv_heads", "head_dim", "block", "prefix_tokens", "reserved", "n_items", "n_planes",
                                               "total_q", "total_k", "kernel")] + \
-               [("cu_q", ctypes.POINTER(ctypes.c_int32)), ("cu_k", ctypes.POINTER(ctypes.c_int32)), ("work", ctypes.c_void_p), ("work_bytes", ctypes.c_size_t)]
+               [("cu_q", ctypes.POINTER(ctypes.c_int32)), ("cu_k", ctypes.POINTER(ctypes.c_int32)), ("work", ctypes.c_void_p), ("work_bytes", ctypes.c_size_t),
+                ("planned_for", ctypes.c_uint64)]
 
 
 _lib = None
@@ -468,6 +469,8 @@ def pf_packed_attn_fwd(packed, q, k, v, out, workspace, k_prefix=None, v_prefix=
     if packed.prefix_tokens:
         pl = _packed_layout(KV, packed.prefix_tokens, D, dev, k_prefix, v_prefix)
         kp, vp = k_prefix.data_ptr(), v_prefix.data_ptr()
+    else:
+        assert k_prefix is None and v_prefix is None
     ws = ws_bytes = 0
     if workspace is not None:
         assert workspace.get_device() == dev and workspace.is_contiguous()

@@ -132,7 +132,7 @@ struct PackedTile {
   static __device__ constexpr int swz_v(int r) { return D == 128 ? (r & 3) << 2 : ((r >> 1) & 1) << 2; }
 };
 
-// n / group by multiplication (n < 2^31; see packed_group): divisions by a number known at run time are some 25 instructions each, and there
+// n / group by multiplication (n < 2^31; the factors are worked out in pf_packed_attn_fwd): divisions by a number known at run time are some 25 instructions each, and there
 // are several for every row of a tile
 __device__ __forceinline__ int packed_div_group(const PackedParams &P, int n) {
   return P.group == 1 ? n : (int)(__umulhi((unsigned)n, P.group_mul) >> P.group_shift);
@@ -1000,7 +1000,8 @@ static double packed_lay_out(const pf_packed *p, const PackedCosts &C, bool take
   return least;
 }
 
-static void packed_make(const pf_packed *p, PackedPlan &plan) {
+constexpr long long PACKED_MAX_ITEMS = (1 << 23) - 1;             // a launch has fewer than 2^32 threads, an item up to 512
+static int packed_make(const pf_packed *p, PackedPlan &plan) {
   PackedLayout L;
   double least = 1e300;
   for (int wide = 0; wide < (p->head_dim == 128 ? 2 : 1); ++wide)
@@ -1014,6 +1015,9 @@ static void packed_make(const pf_packed *p, PackedPlan &plan) {
       }
     }
   plan.planes = L.planes;
+  long long n_items = 0;
+  for (const int n : L.cuts) n_items += (long long)n * p->n_kv_heads;
+  if (n_items > PACKED_MAX_ITEMS) return PF_ERR_UNSUPPORTED;
   struct Loaded {
     PackedItem item;
     int load;
@@ -1045,6 +1049,19 @@ static void packed_make(const pf_packed *p, PackedPlan &plan) {
     for (size_t d = 0; d < PF_NUM_XCD; ++d)
       for (size_t i = a + (d + PF_NUM_XCD - a % PF_NUM_XCD) % PF_NUM_XCD; i < b; i += PF_NUM_XCD) plan.items[i] = items[from++].item;
   }
+  return PF_OK;
+}
+
+// What a plan is for: with anything else its items would point outside the tensors.
+static uint64_t packed_checksum(const pf_packed *p) {
+  uint64_t h = 1469598103934665603ull;                            // FNV-1a, a word at a time
+  auto add = [&](int32_t x) { h = (h ^ (uint32_t)x) * 1099511628211ull; };
+  for (const int32_t x : {p->n_seqs, p->n_heads, p->n_kv_heads, p->head_dim, p->block, p->prefix_tokens, p->n_items, p->n_planes, p->kernel}) add(x);
+  for (int s = 1; s <= p->n_seqs; ++s) add(p->cu_q[s]), add(p->cu_k[s]);
+  return h;
+}
+static bool packed_is_planned(const pf_packed *p) {
+  return p->total_q == p->cu_q[p->n_seqs] && p->total_k == p->cu_k[p->n_seqs] && p->planned_for == packed_checksum(p);
 }
 
 static size_t packed_part_bytes(const pf_packed *p, int planes) {
@@ -1069,7 +1086,8 @@ extern "C" size_t pf_packed_work_bytes(const pf_packed *packed) {
     const int rc = packed_check(packed);
     if (rc != PF_OK) return rc;
     PackedPlan plan;
-    packed_make(packed, plan);
+    const int made = packed_make(packed, plan);
+    if (made != PF_OK) return made;
     n = packed_plan_bytes(plan.items.size(), packed->n_kv_heads);
     return PF_OK;
   });
@@ -1082,7 +1100,8 @@ extern "C" int pf_packed_plan(pf_packed *packed, void *stream) {
     if (rc != PF_OK) return rc;
     if (!packed->work || ((uintptr_t)packed->work & 31u)) return (int)PF_ERR_INVALID_ARG;
     PackedPlan plan;
-    packed_make(packed, plan);
+    const int made = packed_make(packed, plan);
+    if (made != PF_OK) return made;
     if (packed->work_bytes < packed_plan_bytes(plan.items.size(), packed->n_kv_heads)) return (int)PF_ERR_CAPACITY;
     PackedItem *to = (PackedItem *)packed->work;
     for (size_t i = 0; i < plan.items.size(); i += PACKED_UPLOAD) {
@@ -1099,12 +1118,13 @@ extern "C" int pf_packed_plan(pf_packed *packed, void *stream) {
     packed->kernel = plan.wide ? 1 : 0;
     packed->total_q = packed->cu_q[packed->n_seqs];
     packed->total_k = packed->cu_k[packed->n_seqs];
+    packed->planned_for = packed_checksum(packed);
     return (int)PF_OK;
   });
 }
 
 extern "C" size_t pf_packed_workspace_bytes(const pf_packed *packed) {
-  if (packed_check(packed) != PF_OK || packed->n_planes < 0 || packed->n_planes > PACKED_MAX_PLANES) return 0;
+  if (packed_check(packed) != PF_OK || !packed_is_planned(packed)) return 0;
   return pf_align_up(packed_part_bytes(packed, packed->n_planes) + 256, 256);
 }
 
@@ -1115,14 +1135,12 @@ extern "C" int pf_packed_attn_fwd(const pf_packed *packed, const void *q, const 
   const int rc = packed_check(packed);
   if (rc != PF_OK) return rc;
   const int tq = packed->cu_q[packed->n_seqs], tk = packed->cu_k[packed->n_seqs], D = packed->head_dim;
-  if (packed->n_items < 0 || packed->kernel < 0 || packed->kernel > (D == 128 ? 1 : 0) || packed->n_planes < 0 || packed->n_planes > PACKED_MAX_PLANES || packed->total_q != tq || packed->total_k != tk)
-    return PF_ERR_INVALID_ARG;                                    // not planned, or planned for other lengths
-  if (tq > 0 && packed->n_items == 0) return PF_ERR_INVALID_ARG;
+  if (!packed_is_planned(packed)) return PF_ERR_INVALID_ARG;
   if (!packed->work || ((uintptr_t)packed->work & 31u) || packed->work_bytes < packed_plan_bytes(packed->n_items, packed->n_kv_heads)) return PF_ERR_INVALID_ARG;
   if (!(softmax_scale >= 0.0f) || softmax_scale > 1.0e6f) return PF_ERR_INVALID_ARG;
   if (tq > 0 && (!q || !out)) return PF_ERR_INVALID_ARG;
   if (tk > 0 && (!k || !v)) return PF_ERR_INVALID_ARG;
-  if (packed->prefix_tokens > 0 && (!k_prefix || !v_prefix)) return PF_ERR_INVALID_ARG;
+  if (packed->prefix_tokens > 0 ? !k_prefix || !v_prefix : k_prefix || v_prefix) return PF_ERR_INVALID_ARG;
   if ((((uintptr_t)q) | ((uintptr_t)k) | ((uintptr_t)v) | ((uintptr_t)out) | ((uintptr_t)k_prefix) | ((uintptr_t)v_prefix) | ((uintptr_t)workspace)) & 15u)
     return PF_ERR_INVALID_ARG;
   if (!pf_chunk_layout_ok(q_layout, packed->n_heads, tq, D) || !pf_chunk_layout_ok(out_layout, packed->n_heads, tq, D) ||

@@ -219,7 +219,7 @@ static int rope_rows_ok(const pf_rope_rows *t, int n_tokens, int head_dim) {
 
 extern "C" int pf_qk_norm_rope(const pf_rope *rope, int n_tokens, const int32_t *positions, const pf_rope_rows *q, const pf_rope_rows *k,
                                float eps, void *stream) {
-  if (!rope || !q || !k || n_tokens < 0 || n_tokens > (1 << 26)) return PF_ERR_INVALID_ARG;
+  if (!rope || !q || !k || n_tokens < 0 || n_tokens >= (1 << 26)) return PF_ERR_INVALID_ARG;
   const int D = rope->head_dim;
   if (D != 64 && D != 128) return PF_ERR_UNSUPPORTED;
   if (rope->rot_dim < 0 || rope->rot_dim > D || rope->rot_dim % 8 || rope->n_axes < 1 || rope->n_axes > 3) return PF_ERR_INVALID_ARG;

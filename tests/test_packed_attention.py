@@ -61,6 +61,17 @@ def test_plans_refused():
     assert e.value.status == B.PF_ERR_UNSUPPORTED
 
 
+def _checksum(s):
+    """64-bit FNV-1a over the words that a plan depends on."""
+    h = 1469598103934665603
+    words = [s.n_seqs, s.n_heads, s.n_kv_heads, s.head_dim, s.block, s.prefix_tokens, s.n_items, s.n_planes, s.kernel]
+    for i in range(1, s.n_seqs + 1):
+        words += [s.cu_q[i], s.cu_k[i]]
+    for w in words:
+        h = ((h ^ (w & 0xffffffff)) * 1099511628211) % 2 ** 64
+    return h
+
+
 def test_calls_refused_without_a_device():
     """A struct filled in as a plan would (no plan is uploaded: every refusal comes before anything is enqueued)."""
     L, bad, fake = B.lib(), B.PF_ERR_INVALID_ARG, 0x10000
@@ -69,9 +80,10 @@ def test_calls_refused_without_a_device():
         lay = lambda x: None if x is None else ctypes.byref(B.pf_chunk_layout(*x))
         return L.pf_packed_attn_fwd(ctypes.byref(s), q, lay(ql), k, v, lay(kl), kp, vp, lay(pl), out, lay(ql if ol is None else ol), scale, ws, ws_bytes, None)
 
-    def planned(**kw):
+    def planned(planes=0, **kw):
         s = _struct(**kw)
-        s.n_items, s.n_planes, s.total_q, s.total_k = 4, 0, s._keep[0][len(s._keep[0]) - 1], s._keep[1][len(s._keep[1]) - 1]
+        s.n_items, s.n_planes, s.total_q, s.total_k = 4, planes, s._keep[0][len(s._keep[0]) - 1], s._keep[1][len(s._keep[1]) - 1]
+        s.planned_for = _checksum(s)
         return s
 
     assert call(_struct()) == bad                                 # never planned
@@ -88,14 +100,31 @@ def test_calls_refused_without_a_device():
     assert call(s) == bad
     s = planned(work=0)
     assert call(s) == bad
-    s = planned(prefix=10)
-    s.n_planes = 2
+    for field, x in (("n_heads", 2), ("n_kv_heads", 1), ("head_dim", 64), ("block", 2), ("prefix_tokens", 3), ("n_items", 3), ("n_planes", 1), ("kernel", 1)):
+        s = planned()
+        setattr(s, field, x)                                      # planned for something else
+        assert call(s, kp=fake, vp=fake, ws=0x20000, ws_bytes=1 << 30) == bad, field
+        assert L.pf_packed_workspace_bytes(ctypes.byref(s)) == 0
+    s = planned()
+    s._keep[0][1] = s._keep[1][1] = 6                             # other lengths of the same sum, written where the old ones were
+    assert call(s) == bad
+    assert call(planned(), kp=fake) == bad and call(planned(), vp=fake) == bad   # a prefix of no tokens
+    assert L.pf_packed_workspace_bytes(ctypes.byref(_struct())) == 0
+    s = planned(planes=2, prefix=10)
     need = 2 * 9 * 4 * (128 * 4 + 8)
     assert L.pf_packed_workspace_bytes(ctypes.byref(s)) >= need
     assert call(s, ws=0x20000, ws_bytes=need) == bad              # no prefix tensors
     assert call(s, kp=fake, vp=fake, pl=(256, 128)) == bad        # no workspace
     assert call(s, kp=fake, vp=fake, pl=(256, 128), ws=0x20000, ws_bytes=need - 1) == bad
     assert call(s, kp=fake, vp=fake, pl=(128, 128), ws=0x20000, ws_bytes=need) == bad
+
+
+def test_batches_of_too_many_items_are_refused():
+    """8 heads of 2^20 sequences: a launch of 2^23 workgroups would have too many threads."""
+    n = 1 << 20
+    s, L = _struct(cu_q=tuple(range(n + 1)), cu_k=tuple(range(n + 1)), heads=8, kv=8), B.lib()
+    assert L.pf_packed_work_bytes(ctypes.byref(s)) == 0
+    assert L.pf_packed_plan(ctypes.byref(s), None) == B.PF_ERR_UNSUPPORTED
 
 
 def test_tensors_of_another_device_are_refused():
@@ -276,6 +305,88 @@ def test_masked_keys_do_not_count(bad, D):
     k[:, 77:] = bad
     got = _run(cu, cu, q, k, v, 1)
     assert torch.equal(got[:, :77], out[:, :77])
+
+
+def _wide(lq, lk, G, block, P=0):
+    """The first number of key heads that the planner takes wide items for."""
+    for KV in range(8, 65, 4):
+        packed = B.Packed(_cu(lq), _cu(lk), KV * G, KV, 128, block=block, prefix_tokens=P, device=DEV)
+        B.pf_packed_plan(packed)
+        if packed.c.kernel == 1:
+            return KV
+    raise AssertionError("the case must go by wide items")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bad", [float("nan"), -float("inf"), -3.0e38])
+def test_masked_keys_do_not_count_in_wide_items(bad):
+    lq = [1200]
+    KV, cu = _wide(lq, lq, 1, 1), _cu(lq)
+    q, k, v, _, _ = _tensors(KV, KV, 128, 1200, 1200, 0, 13, True)
+    out = _run(cu, cu, q, k, v, 1)
+    k[:, 777:] = bad
+    got = _run(cu, cu, q, k, v, 1)
+    assert torch.equal(got[:, :777], out[:, :777])
+
+
+@pytest.mark.gpu
+def test_rows_behind_the_last_sequence_of_wide_items():
+    lq = [1100, 77]
+    KV, cu, n = _wide(lq, lq, 2, 1), _cu(lq), 1177
+    q, k, v, _, _ = _tensors(2 * KV, KV, 128, n, n, 0, 19, True, spare=300)
+    k[:, n:], v[:, n:] = float("nan"), float("inf")
+    out = _run(cu, cu, q, k, v, 1)
+    want, tol = _definition(q[:, :n], k[:, :n], v[:, :n], cu, cu, 1)
+    assert ((out[:, :n].double() - want).abs() <= tol).all() and torch.isnan(out[:, n:]).all()
+
+
+@pytest.mark.gpu
+def test_wide_items_beyond_32_bits():
+    """Sequences behind one of 1 100 000 keys (and no query): they lie beyond 2^32 bytes of K and V."""
+    lq, lk, D = [0, 1100, 77], [1100000, 1100, 77], 128
+    KV = _wide(lq, lk, 2, 1)
+    assert 1100000 * KV * D * 2 > 2 ** 32
+    g = torch.Generator(device=DEV)
+    g.manual_seed(3)
+    k = torch.empty((sum(lk), KV, D), dtype=torch.bfloat16, device=DEV)
+    v = torch.empty_like(k)
+    for t in (k, v):
+        for i in range(0, sum(lk), 50000):
+            t[i:i + 50000] = torch.randn(t[i:i + 50000].shape, generator=g, device=DEV).to(torch.bfloat16)
+    k, v = k.transpose(0, 1), v.transpose(0, 1)
+    q = synth.randn_bf16((sum(lq), 2 * KV, D), 5, device=DEV).transpose(0, 1)
+    out = _run(_cu(lq), _cu(lk), q, k, v, 1)
+    want, tol = _definition(q, k, v, _cu(lq), _cu(lk), 1)
+    assert ((out.double() - want).abs() <= tol).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("D", [64, 128])
+def test_more_planes_than_a_wave_has_lanes(D):
+    cu_q, cu_k = _cu([1]), _cu([40001])
+    packed = B.Packed(cu_q, cu_k, 40, 1, D, block=1, device=DEV)
+    B.pf_packed_plan(packed)
+    assert packed.c.n_planes > 64, "the case must park many partial results"
+    _case(cu_q, cu_k, 40, 1, D, 1, 0, seed=23)
+
+
+@pytest.mark.gpu
+def test_lengths_that_change_need_a_plan():
+    """The lengths of a batch written over in place: refused until planned again, right afterwards."""
+    packed = B.Packed(_cu([70, 30]), _cu([70, 30]), 4, 2, 64, block=1, device=DEV)
+    q, k, v, _, _ = _tensors(4, 2, 64, 100, 100, 0, 29, True)
+    out = torch.empty_like(q)
+    B.pf_packed_plan(packed)
+    ws = torch.empty(1 << 22, dtype=torch.uint8, device=DEV)
+    B.pf_packed_attn_fwd(packed, q, k, v, out, ws)
+    packed.cu_q[1] = packed.cu_k[1] = 20
+    with pytest.raises(B.PfError):
+        B.pf_packed_attn_fwd(packed, q, k, v, out, ws)
+    B.pf_packed_plan(packed)
+    assert B.pf_packed_workspace_bytes(packed) <= ws.numel()
+    B.pf_packed_attn_fwd(packed, q, k, v, out, ws)
+    want, tol = _definition(q, k, v, [0, 20, 100], [0, 20, 100], 1)
+    assert ((out.double() - want).abs() <= tol).all()
 
 
 @pytest.mark.gpu

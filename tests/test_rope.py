@@ -88,7 +88,7 @@ def test_calls_refused_without_a_device():
     empty = B.pf_rope_rows()
     bad = B.PF_ERR_INVALID_ARG
     assert call(n=0) == B.PF_OK                                   # nothing to do, nothing touched
-    assert call(n=-1) == bad and call(n=(1 << 26) + 1) == bad
+    assert call(n=-1) == bad and call(n=1 << 26) == bad and call(n=(1 << 26) + 1) == bad
     assert call(r=None) == bad and call(p=None) == bad and call(p=ctypes.c_void_p(0x1002)) == bad
     assert L.pf_qk_norm_rope(ctypes.byref(rope), 10, pos, None, ctypes.byref(rows()), 1e-6, None) == bad
     assert call(q=empty, k=empty) == bad
