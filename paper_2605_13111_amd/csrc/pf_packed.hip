@@ -208,9 +208,9 @@ struct PackedRow {
 __device__ __forceinline__ float packed_mc(float m, float c) { return fmaxf(m * c, -3.0e38f); }
 
 // Scores of NKB blocks of 32 keys (accumulators of K Q^T: register i of block kb is key 32 kb + 8 (i / 4) + 4 g + i % 4) -> weights in bf16,
-// the row's state and O moved on.
+// the row's state and O moved on.  first: an item's first tile, whose rows have no reference yet.
 template <int D, int NKB>
-__device__ __forceinline__ void packed_softmax(f32x16 (&s)[NKB], bf16x8 (&pf)[2 * NKB], f32x16 (&o)[D / 32], PackedRow &R, float c) {
+__device__ __forceinline__ void packed_softmax(f32x16 (&s)[NKB], bf16x8 (&pf)[2 * NKB], f32x16 (&o)[D / 32], PackedRow &R, float c, bool first) {
   float ts[2];
   auto weights = [&]() __attribute__((always_inline)) {
 #pragma unroll
@@ -224,7 +224,13 @@ __device__ __forceinline__ void packed_softmax(f32x16 (&s)[NKB], bf16x8 (&pf)[2 
         pf[kb * 2 + (i >> 3)][(i & 7) + 1] = (__bf16)e1;
       }
   };
-  weights();
+  if (__builtin_expect(!first, 1)) {
+    weights();
+  } else {                                                        // as if they had been formed against no reference at all
+    ts[0] = ts[1] = INFINITY;
+#pragma unroll
+    for (int i = 0; i < 2 * NKB; ++i) pf[i] = bf16x8{};
+  }
 #pragma unroll
   for (int i = 0; i < 2 * NKB; ++i) asm volatile("" : "+v"(pf[i]));   // rounded here: sunk past the branch, all weights would stay in registers
   if (__builtin_expect(tile_sum_too_large(ts[0] + ts[1]), 0)) {
@@ -317,6 +323,39 @@ __device__ __forceinline__ void packed_load_q(const PackedParams &P, const Packe
 #pragma unroll
   for (int ks = 0; ks < D / 16; ++ks) qf[ks] = *(const bf16x8 *)(q + ks * 16);
 }
+// The same of a wave's 32 rows, through 32 rows of LDS that are its own: a load of Q^T fragments from memory touches 32 rows (64 cycles for 1 KB), a
+// copy of whole rows 4 or 8.  First the copies, ...
+template <int D>
+__device__ __forceinline__ void packed_send_q(const PackedParams &P, const PackedItem &it, int wrow0, char *stage, int lane) {
+  typedef PackedTile<D> C;
+  typedef __attribute__((address_space(3))) void *lptr_t;
+  typedef const __attribute__((address_space(1))) void *gptr_t;
+  asm volatile("" : "+v"(lane));
+  const int row = pf_min(wrow0 + (lane & 31), it.n_rows - 1), t = packed_div_group(P, row), h = packed_head(it) * P.group + row - t * P.group;
+  const unsigned long long q = (unsigned long long)(P.q + (it.q_base + t) * P.q_tok + h * P.q_head);
+  const int r0 = lane / C::CHUNKS, p = lane % C::CHUNKS;
+  static_for<0, 32 / C::COPY_ROWS>([&](auto gi) {
+    constexpr int G = decltype(gi)::value;
+    const int r = G * C::COPY_ROWS + r0;
+    const unsigned lo = __builtin_amdgcn_ds_bpermute(r * 4, (int)(unsigned)q), hi = __builtin_amdgcn_ds_bpermute(r * 4, (int)(unsigned)(q >> 32));
+    __builtin_amdgcn_global_load_lds((gptr_t)(((unsigned long long)hi << 32 | lo) + ((p ^ C::swz_k(r)) << 4)), (lptr_t)(stage + G * 1024), 16, 0, 0);
+  });
+}
+// ... and once they have landed, the fragments.
+template <int D>
+__device__ __forceinline__ void packed_read_q(const char *stage, int lane, bf16x8 (&qf)[D / 16]) {
+  typedef PackedTile<D> C;
+  unsigned aq, unused;
+  packed_lds<D>(stage, stage, lane, aq, unused);
+  u32x4 x[C::NKS];
+  static_for<0, C::NKS>([&](auto i) { read_k<0>(x[decltype(i)::value], aq ^ (unsigned)(decltype(i)::value << 5)); });
+  wait_lds<0>();
+#pragma unroll
+  for (int ks = 0; ks < C::NKS; ++ks) {
+    asm volatile("" : "+v"(x[ks]));
+    qf[ks] = __builtin_bit_cast(bf16x8, x[ks]);
+  }
+}
 // Partial results that the head's last workgroup joins cross workgroups on different dies, each with an L2 of its own: they are written and read
 // at device scope, 8 bytes at a time, past the L2; the wait for the stores before the arrival is all that stands between.
 __device__ __forceinline__ void packed_st8(void *p, float a, float b) {
@@ -382,7 +421,7 @@ __device__ __forceinline__ void packed_put(const PackedTo<D> &to, int d0, const 
 }
 // The workgroup is done with its item.  Where there is no second kernel, the last one of its head joins the planes of the head's rows (see
 // pf_packed_join_few_kernel): D / 8 lanes take a row, four planes in flight.  Bound: the round trips to memory, one per four planes.
-template <int D, int WAVES>
+template <int D>
 __device__ __forceinline__ void packed_arrive(const PackedItem &it, int32_t *s_last, int tid) {
   const PackedParams P = packed_params();
   if (P.arrivals == nullptr) return;
@@ -408,7 +447,7 @@ __device__ __forceinline__ void packed_arrive(const PackedItem &it, int32_t *s_l
 #endif
   constexpr int LANES = D / 8, AHEAD = 4;
   const int n = P.n_rows / P.n_heads * P.group, d0 = tid % LANES * 8;
-  for (int r = tid / LANES; r < n; r += WAVES * 64 / LANES) {
+  for (int r = tid / LANES; r < n; r += PACKED_WAVES * 64 / LANES) {
     const int t = packed_div_group(P, r), h = head * P.group + r - t * P.group;
     const long long id = (long long)t * P.n_heads + h;
     float top = -3.0e38f, sum = 0.0f, acc[8] = {};
@@ -497,13 +536,14 @@ __device__ __forceinline__ void packed_full(const PackedItem &it, char *smem, in
   const int l32 = lane & 31, g = lane >> 5, n_tiles = it.kt1 - it.kt0;
   const int wrow0 = it.row0 + wave * 32;
   const bool has_rows = wrow0 < it.n_rows;
+  char *const stage_q = smem + C::STAGE_BYTES + wave * (32 * C::ROW_BYTES);   // in the second tile's stage, whose copies go out behind a barrier
   bf16x8 qf[C::NKS];
   int pre, prefix_tokens, limit;                                  // the prefix's tiles and keys, if the line has it; this lane's row sees so many own keys
   float c;
   {
     const PackedParams P = packed_params();
     const int row = pf_min(wrow0 + l32, it.n_rows - 1);
-    packed_load_q<D>(P, it, row, g, qf);                          // first: what waits for it does not wait for the copies behind it
+    packed_send_q<D>(P, it, wrow0, stage_q, lane);
     pre = packed_has_prefix(it) ? P.prefix_tiles : 0;
     prefix_tokens = P.prefix_tokens;
     limit = packed_limit(P, it, row);
@@ -560,8 +600,9 @@ __device__ __forceinline__ void packed_full(const PackedItem &it, char *smem, in
   copy_tile(0);
   // the limit grows with the row: the wave's first lane has the least, its 32nd the most
   const int lim_first = __builtin_amdgcn_readlane(limit, 0), lim_last = __builtin_amdgcn_readlane(limit, 31);
-#pragma unroll
-  for (int ks = 0; ks < C::NKS; ++ks) asm volatile("" : "+v"(qf[ks]));   // the compiler waits here, not inside the loop
+  if (n_tiles > 0) wait_vm<2 * NC>();                             // the first tile may still travel
+  else wait_vm<0>();
+  packed_read_q<D>(stage_q, lane, qf);
   f32x16 o[C::NDB];
 #pragma unroll
   for (int db = 0; db < C::NDB; ++db)
@@ -582,7 +623,7 @@ __device__ __forceinline__ void packed_full(const PackedItem &it, char *smem, in
     if (__builtin_expect((kt < pre ? prefix_tokens : lim_first) - t0 < PF_BK, 0))   // some row does not see the whole tile
       packed_mask<2>(s, (kt < pre ? prefix_tokens : limit) - t0, g);
     bf16x8 pf[4];
-    packed_softmax<D, 2>(s, pf, o, R, c);
+    packed_softmax<D, 2>(s, pf, o, R, c, u == 0);
     packed_pv<D, 4>(o, pf, av + stage);
   }
   packed_results<D>(it, wrow0, o, R, lane);
@@ -630,7 +671,7 @@ __device__ __forceinline__ void packed_thin(const PackedItem &it, char *smem, fl
       if (__builtin_expect((kt < K.pre ? P.prefix_tokens : lim_first) - t0 < KEYS, 0))
         packed_mask<1>(s, (kt < K.pre ? P.prefix_tokens : limit) - t0, g);
       bf16x8 pf[2];
-      packed_softmax<D, 1>(s, pf, o, R, c);
+      packed_softmax<D, 1>(s, pf, o, R, c, j == j0);
       if (more) wait_vm<NC>();                                    // V of this step has landed (K of the next may still travel)
       else wait_vm<0>();
       packed_pv<D, 2>(o, pf, av);
@@ -669,10 +710,14 @@ __global__ __launch_bounds__(PACKED_WAVES * 64, 2 * 128 / D) void pf_packed_attn
   __shared__ float2 s_ml[PACKED_WAVES * 32];
   __shared__ int32_t s_last;
   const PackedItem it = packed_item();
-  if (packed_is_thin(it)) packed_thin<D>(it, smem, s_ml, threadIdx.x);
-  else packed_full<D>(it, smem, threadIdx.x);
-  packed_arrive<D, PACKED_WAVES>(it, &s_last, threadIdx.x);
+  if (!packed_is_thin(it)) {
+    packed_full<D>(it, smem, threadIdx.x);
+    return;
+  }
+  packed_thin<D>(it, smem, s_ml, threadIdx.x);
+  packed_arrive<D>(it, &s_last, threadIdx.x);                     // (a head of few rows has thin items only)
 }
+static_assert(PACKED_ARRIVE_ROWS <= PACKED_THIN_ROWS, "full and wide items have no arrivals");
 
 #include "pf_packed_wide.h"
 
@@ -1004,7 +1049,7 @@ constexpr long long PACKED_MAX_ITEMS = (1 << 23) - 1;             // a launch ha
 static int packed_make(const pf_packed *p, PackedPlan &plan) {
   PackedLayout L;
   double least = 1e300;
-  for (int wide = 0; wide < (p->head_dim == 128 ? 2 : 1); ++wide)
+  for (int wide = 0; wide < (p->head_dim == 128 && !packed_by_arrival(p) ? 2 : 1); ++wide)
     for (int take_all = 0; take_all < (p->prefix_tokens > 0 ? 2 : 1); ++take_all) {
       PackedLayout other;
       const double t = packed_lay_out(p, packed_costs(p->head_dim, wide != 0), take_all != 0, other);

@@ -36,13 +36,16 @@ __device__ __forceinline__ void packed_wide(const PackedItem &it, char *smem, in
   const int l32 = lane & 31, g = lane >> 5, n_tiles = it.kt1 - it.kt0;
   const int wrow0 = it.row0 + wave * 32;
   char *const ring_k = smem + wave * (WROWS * C::ROW_BYTES), *const ring_v = ring_k + WIDE_KSTAGES * WIDE_TILE;
+  // where its queries are staged: what K of tiles 2 and 3 and V of tiles 3 and 4 will take
+  char *const stage_q = smem + (wave < 4 ? 2 * WIDE_TILE : (WIDE_KSTAGES + 1) * WIDE_TILE) + wave * (32 * C::ROW_BYTES);
+  static_assert(WIDE_WAVES == 8 && WIDE_KSTAGES == 4 && WIDE_VSTAGES == 5, "two stages of K and of V hold four waves' queries each");
   bf16x8 qf[C::NKS];
   int pre, prefix_tokens, limit;                                  // the prefix's tiles and keys, if the line has it; this lane's row sees so many own keys
   float c;
   {
     const PackedParams P = packed_params();
     const int row = pf_min(wrow0 + l32, it.n_rows - 1);
-    packed_load_q<D>(P, it, row, g, qf);
+    packed_send_q<D>(P, it, wrow0, stage_q, lane);
     pre = packed_has_prefix(it) ? P.prefix_tiles : 0;
     prefix_tokens = P.prefix_tokens;
     limit = packed_limit(P, it, row);
@@ -102,14 +105,20 @@ __device__ __forceinline__ void packed_wide(const PackedItem &it, char *smem, in
     else wait_vm<0>();
   };
 #pragma unroll 1
-  for (int i = 0; i < 3; ++i) copy_tile(i, i * WIDE_TILE, i * WIDE_TILE, []() {});
+  for (int i = 0; i < 3; ++i) {
+    if (i == 2) {                                                 // some of its place holds queries until here
+      if (n_tiles > 1) wait_vm<2 * NC>();                         // queries and the first tile have landed
+      else wait_vm<0>();
+      packed_read_q<D>(stage_q, lane, qf);
+      __builtin_amdgcn_s_barrier();
+    }
+    copy_tile(i, i * WIDE_TILE, i * WIDE_TILE, []() {});
+  }
 
   // the limit grows with the row: the wave's first lane has the least, its 32nd the most.  A wave computes its tiles up to the last that one of
   // its rows sees; behind it it sends its copies and meets the barriers, and does nothing else.
   const int lim_first = __builtin_amdgcn_readlane(limit, 0), lim_last = __builtin_amdgcn_readlane(limit, 31);
   const int mine = wrow0 < it.n_rows ? pf_max(0, pf_min(n_tiles, pre + pf_ceil_div(lim_last, PF_BK) - it.kt0)) : 0;
-#pragma unroll
-  for (int ks = 0; ks < C::NKS; ++ks) asm volatile("" : "+v"(qf[ks]));
   f32x16 o[C::NDB];
 #pragma unroll
   for (int db = 0; db < C::NDB; ++db)
@@ -118,8 +127,6 @@ __device__ __forceinline__ void packed_wide(const PackedItem &it, char *smem, in
   PackedRow R = {-3.0e38f, 0.0f, packed_mc(-3.0e38f, c)};
   unsigned ak, av;
   packed_lds<D>(smem, smem + WIDE_KSTAGES * WIDE_TILE, lane, ak, av);
-  wait_vm<0>();
-  __builtin_amdgcn_s_barrier();
   if (grp == 1) __builtin_amdgcn_s_barrier();                     // group 1 trails by one phase
 
   // ---- a matrix phase consumes 32 operand fragments from LDS, one per MFMA:
@@ -171,11 +178,11 @@ __device__ __forceinline__ void packed_wide(const PackedItem &it, char *smem, in
     asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(vl[0]), "+v"(vh[0]), "+v"(vl[1]), "+v"(vh[1]), "+v"(vl[2]), "+v"(vh[2]), "+v"(vl[3]), "+v"(vh[3]), "+v"(vl[4]), "+v"(vh[4]));
   };
   static_assert(WIDE_RING == 5, "settle names the fragments in flight");
-  auto weights = [&](int u) __attribute__((always_inline)) {
+  auto weights = [&](int u, bool first) __attribute__((always_inline)) {
     const int kt = it.kt0 + u, t0 = (kt < pre ? kt : kt - pre) * PF_BK;
     if (__builtin_expect((kt < pre ? prefix_tokens : lim_first) - t0 < PF_BK, 0))   // some row does not see the whole tile
       packed_mask<2>(s, (kt < pre ? prefix_tokens : limit) - t0, g);
-    packed_softmax<D, 2>(s, pf, o, R, c);
+    packed_softmax<D, 2>(s, pf, o, R, c, first);
   };
   // ring offsets of tile u (ok, ov) and of the V tiles before it (ov1, ov2)
   unsigned ok = 0, ov = 0, ov1 = (WIDE_VSTAGES - 1) * WIDE_TILE, ov2 = (WIDE_VSTAGES - 2) * WIDE_TILE;
@@ -190,9 +197,12 @@ __device__ __forceinline__ void packed_wide(const PackedItem &it, char *smem, in
   };
   int u = 1;
   if (__builtin_expect(mine > 0, 1)) {
-    m_phase(IntC<0>(), IntC<1>(), 0, 0, 0, []() __attribute__((always_inline)) { __builtin_amdgcn_s_barrier(); });
+    m_phase(IntC<0>(), IntC<1>(), 0, 0, 0, [&]() __attribute__((always_inline)) {
+      wait_copies(2);
+      __builtin_amdgcn_s_barrier();
+    });
     copy_next(0, settle);
-    weights(0);
+    weights(0, true);
     __builtin_amdgcn_s_barrier();
     for (; u < mine; ++u) {
       rings_on();
@@ -202,7 +212,7 @@ __device__ __forceinline__ void packed_wide(const PackedItem &it, char *smem, in
         __builtin_amdgcn_s_barrier();
       });
       copy_next(u, settle);
-      weights(u);
+      weights(u, false);
       __builtin_amdgcn_s_barrier();
     }
     // the values of the wave's last tile: its matrix phase of the tile behind it, or the item's last
@@ -211,6 +221,7 @@ __device__ __forceinline__ void packed_wide(const PackedItem &it, char *smem, in
       __builtin_amdgcn_s_barrier();
     });
   } else {
+    wait_copies(2);
     __builtin_amdgcn_s_barrier();
     u = 0;
   }
@@ -238,10 +249,7 @@ __device__ __forceinline__ void packed_wide(const PackedItem &it, char *smem, in
 
 __global__ __launch_bounds__(WIDE_WAVES * 64, 2) void pf_packed_wide_kernel(PackedParams) {
   __shared__ __attribute__((aligned(1024))) char smem[(WIDE_KSTAGES + WIDE_VSTAGES) * WIDE_TILE];
-  __shared__ int32_t s_last;
-  const PackedItem it = packed_item();
-  packed_wide(it, smem, threadIdx.x);
-  packed_arrive<128, WIDE_WAVES>(it, &s_last, threadIdx.x);
+  packed_wide(packed_item(), smem, threadIdx.x);
 }
 
 #endif  // PF_PACKED_WIDE_H
