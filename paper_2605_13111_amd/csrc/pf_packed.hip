@@ -500,28 +500,61 @@ __device__ __forceinline__ void packed_stage(float *row, const f32x16 (&o)[D / 3
       *(f32x4 *)(row + db * 32 + 8 * i4 + 4 * g) = f32x4{o[db][i4 * 4], o[db][i4 * 4 + 1], o[db][i4 * 4 + 2], o[db][i4 * 4 + 3]};
 }
 
-// A wave's results straight from the accumulators.  A lane holds four channels of every eight, the other half of the wave the other four: pairs
-// of quads are exchanged, after which a lane has eight channels side by side (16 bytes of the result).  Through LDS, as full rows, this
-// end of an item took 3 us instead of 1 (two barriers, and eight rounds of address arithmetic per thread).
+// A wave's results, through 32 rows of D * 2 bytes of LDS that are its own: a lane of the accumulators has one row, so that a store straight from
+// them would touch 64 cache lines, and as full rows it touches 8 or 16.  Partial results, twice as wide, go in two halves.  No barrier; chunks
+// are permuted as K's.  A prompt of 14040 tokens 680 -> 672 us; short launches are as they were.
 template <int D>
-__device__ __forceinline__ void packed_results(const PackedItem &it, int wrow0, const f32x16 (&o)[D / 32], const PackedRow &R, int lane) {
+__device__ __forceinline__ void packed_results(const PackedItem &it, int wrow0, const f32x16 (&o)[D / 32], const PackedRow &R, char *stage, int lane) {
+  typedef PackedTile<D> C;
+  asm volatile("" : "+v"(lane));                                  // what follows from it is not held in registers through the loop over the tiles
   const int l32 = lane & 31, g = lane >> 5;
   const float lsum = partner_sum(R.l);
-  const bool valid = wrow0 + l32 < it.n_rows;                     // (of no lane, where the wave has no rows)
-  const PackedTo<D> to = packed_to<D>(packed_params(), it, pf_min(wrow0 + l32, it.n_rows - 1), make_float2(R.m, lsum), valid && g == 0);
+  const PackedTo<D> to = packed_to<D>(packed_params(), it, pf_min(wrow0 + l32, it.n_rows - 1), make_float2(R.m, lsum), wrow0 + l32 < it.n_rows && g == 0);
+  char *const mine = stage + l32 * C::ROW_BYTES;
+  const unsigned swz = C::swz_k(l32);
+  // the staged rows to where lanes 0 .. 31 say, 16 bytes a lane
+  auto store = [&](const void *where) __attribute__((always_inline)) {
+    const unsigned long long w = (unsigned long long)where;
+    const int r0 = lane / C::CHUNKS, p = lane % C::CHUNKS;
 #pragma unroll
-  for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-    for (int pair = 0; pair < 2; ++pair) {
-      f32x4 x, y;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_int(o[db][pair * 8 + i]), __float_as_int(o[db][pair * 8 + 4 + i]), false, false);
-        x[i] = __int_as_float(r[0]);
-        y[i] = __int_as_float(r[1]);
-      }
-      if (valid) packed_put<D>(to, db * 32 + (2 * pair + g) * 8, x, y);
+    for (int i = 0; i < 32 / C::COPY_ROWS; ++i) {
+      const int r = i * C::COPY_ROWS + r0;
+      const u32x4 x = *(const u32x4 *)(stage + r * C::ROW_BYTES + ((p ^ C::swz_k(r)) << 4));
+      const unsigned lo = __builtin_amdgcn_ds_bpermute(r * 4, (int)(unsigned)w), hi = __builtin_amdgcn_ds_bpermute(r * 4, (int)(unsigned)(w >> 32));
+      if (wrow0 + r < it.n_rows) *(u32x4 *)packed_global((char *)((unsigned long long)hi << 32 | lo) + 16 * p) = x;
     }
+  };
+  if (packed_plane(it) < 0) {
+    // a lane holds four channels of every eight, the other half of the wave the other four: pairs of quads are exchanged, after which a lane
+    // has eight channels side by side
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int pair = 0; pair < 2; ++pair) {
+        bf16x8 w;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const auto r = __builtin_amdgcn_permlane32_swap(__float_as_int(o[db][pair * 8 + i]), __float_as_int(o[db][pair * 8 + 4 + i]), false, false);
+          w[i] = (__bf16)(__int_as_float(r[0]) * to.inv);
+          w[i + 4] = (__bf16)(__int_as_float(r[1]) * to.inv);
+        }
+        *(bf16x8 *)(mine + (((unsigned)(db * 4 + 2 * pair + g) ^ swz) << 4)) = w;
+      }
+    store(to.out);
+  } else {
+    constexpr int HALF = D / 64;                                  // channel blocks of a half
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+      for (int db = 0; db < HALF; ++db)
+#pragma unroll
+        for (int i4 = 0; i4 < 4; ++i4) {
+          const f32x16 &x = o[h * HALF + db];
+          *(f32x4 *)(mine + (((unsigned)(db * 8 + 2 * i4 + g) ^ swz) << 4)) = f32x4{x[i4 * 4], x[i4 * 4 + 1], x[i4 * 4 + 2], x[i4 * 4 + 3]};
+        }
+      store(to.part + h * (D / 2));
+    }
+  }
 }
 
 // ---- a full item: 128 rows, 32 a wave; the waves share every key tile, two stages of tiles copied global -> LDS directly ----
@@ -626,7 +659,8 @@ __device__ __forceinline__ void packed_full(const PackedItem &it, char *smem, in
     packed_softmax<D, 2>(s, pf, o, R, c, u == 0);
     packed_pv<D, 4>(o, pf, av + stage);
   }
-  packed_results<D>(it, wrow0, o, R, lane);
+  // the stage of the tile before the last: every wave is done with it
+  packed_results<D>(it, wrow0, o, R, smem + (n_tiles & 1) * C::STAGE_BYTES + wave * (32 * C::ROW_BYTES), lane);
 }
 
 // ---- a thin item: 32 rows that all waves hold, the keys split over the waves.  Each streams steps of 32 keys through a place of its own in

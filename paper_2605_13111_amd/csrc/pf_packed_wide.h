@@ -243,8 +243,9 @@ __device__ __forceinline__ void packed_wide(const PackedItem &it, char *smem, in
     }
     __builtin_amdgcn_s_barrier();                                 // the others' last matrix phase
   }
-  if (grp == 0) __builtin_amdgcn_s_barrier();                     // group 0 waits for group 1's last phase
-  packed_results<D>(it, wrow0, o, R, lane);
+  // K's ring: the last phase, in which group 1 may still be, reads V only
+  packed_results<D>(it, wrow0, o, R, smem + wave * (32 * C::ROW_BYTES), lane);
+  if (grp == 0) __builtin_amdgcn_s_barrier();                     // group 1's last phase has one more
 }
 
 __global__ __launch_bounds__(WIDE_WAVES * 64, 2) void pf_packed_wide_kernel(PackedParams) {
