@@ -393,13 +393,15 @@ typedef struct pf_packed {
   uint64_t planned_for;           /* [lib] checksum of the lengths, heads, block and prefix that the plan is for, and of the plan's own sizes */
 } pf_packed;
 
-/* Bytes of pf_packed.work that pf_packed_plan needs for these lengths; 0 on a bad argument.  Host only. */
+/* Bytes of pf_packed.work that pf_packed_plan needs: room for any plan of these heads and query lengths (it does not depend on the
+ * keys, and more queries never need less, so one buffer may serve a batch whose sequences grow).  0 on a bad argument, and for
+ * more than 2^23 - 1 work items.  Host only. */
 size_t pf_packed_work_bytes(const pf_packed *packed);
 
 /* Plan the batch: what pf_packed_attn_fwd does for these lengths, heads and block, for any number of calls (the layers of a
  * model).  Writes `work` on the stream (captured into a graph, a replay writes the same plan again).  A change of lengths, heads,
  * head_dim, block or prefix needs a plan of its own: until then the calls below refuse the batch.
- * PF_ERR_CAPACITY if work_bytes is too small; PF_ERR_UNSUPPORTED if the batch is more than 2^23 - 1 work items. */
+ * PF_ERR_CAPACITY if work_bytes is too small; PF_ERR_UNSUPPORTED where that is 0 for its work items. */
 int pf_packed_plan(pf_packed *packed, void *stream);
 
 /* Bytes of workspace that pf_packed_attn_fwd needs under the plan (partial results of rows whose keys are split); 0 on a bad

@@ -887,6 +887,16 @@ static int packed_host_limit(const pf_packed *p, int lq, int lk, int query) {
 
 // Plan in pf_packed.work: items, then the heads' arrival counters.
 static size_t packed_plan_bytes(size_t items, int kv_heads) { return items * sizeof(PackedItem) + pf_align_up((size_t)kv_heads * sizeof(int32_t), sizeof(PackedItem)); }
+// Room for the plan of any lengths with so many row tiles: theirs and those of stacked lines uncut, and as many items again as several rounds of
+// every place on the chip.  The planner looks at no cut that has more (it would pay for their set-up 16 times over).
+constexpr long long PACKED_CUT_ITEMS = 8192;
+constexpr long long PACKED_MAX_ITEMS = (1 << 23) - 1;             // a launch has fewer than 2^32 threads, an item up to 512
+static long long packed_most_items(const pf_packed *p) {
+  const int G = p->n_heads / p->n_kv_heads;
+  long long tiles = 0;
+  for (int s = 0; s < p->n_seqs; ++s) tiles += pf_ceil_div((long long)(p->cu_q[s + 1] - p->cu_q[s]) * G, PACKED_ROWS);
+  return (p->prefix_tokens > 0 ? 2 : 1) * tiles * p->n_kv_heads + PACKED_CUT_ITEMS;
+}
 // Few rows a head: its last workgroup joins them and there is no second launch.
 static bool packed_by_arrival(const pf_packed *p) { return (long long)p->cu_q[p->n_seqs] * (p->n_heads / p->n_kv_heads) <= PACKED_ARRIVE_ROWS; }
 
@@ -1025,22 +1035,29 @@ static double packed_lay_out(const pf_packed *p, const PackedCosts &C, bool take
   std::stable_sort(tiles.begin(), tiles.end(), [](const PackedRowTile &a, const PackedRowTile &b) { return a.load > b.load; });
   const int longest = tiles.empty() ? 1 : std::max(1, tiles[0].load);
   // A row's planes: its stacked line's first, then its own line's (every tile of a stacked line is cut alike, so that own planes start at one place).
-  auto stack_cuts = [&](int line, int seg) { return std::max(1, std::min(pf_ceil_div(load_of(pre_kt, 0, lines[line]), seg), pre_kt)); };
+  std::vector<int> stack_load(lines.size(), 0);
+  for (size_t l = 0; l < lines.size(); ++l)
+    if (lines[l].stack == -2) stack_load[l] = load_of(pre_kt, 0, lines[l]);
+  auto stack_cuts = [&](int line, int seg) { return std::max(1, std::min(pf_ceil_div(stack_load[line], seg), pre_kt)); };
   auto cuts_of = [&](const PackedCut &cut, size_t i) {
     return lines[tiles[i].line].stack == -2 ? stack_cuts(tiles[i].line, cut.seg) : cut.of((int)i, tiles[i]);
   };
+  long long n_items = 0;
   auto planes_of = [&](const PackedCut &cut, double *parked) {
     int most = 0;
     *parked = 0.0;
+    n_items = 0;
     for (size_t i = 0; i < tiles.size(); ++i) {
       const PackedLine &l = lines[tiles[i].line];
       const int n = cuts_of(cut, i), before = l.stack >= 0 ? stack_cuts(l.stack, cut.seg) : 0;
+      n_items += (long long)n * KV;
       if (l.stack == -1 && n == 1) continue;
       most = std::max(most, before + n);
       *parked += (double)n * pf_min(BQ, l.n_rows - tiles[i].row0);
     }
     return most;
   };
+  const long long most_items = packed_most_items(p);
   PackedCut best = {0, longest};
   double parked = 0.0, least = 1e300;
   if ((long long)tiles.size() * KV <= 8ll * C.places) {
@@ -1051,7 +1068,7 @@ static double packed_lay_out(const pf_packed *p, const PackedCosts &C, bool take
       for (int n : {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 40, 48, 64, 80, 96, 120}) {
         const PackedCut cut = {whole, pf_ceil_div(most, n)};
         const int planes = planes_of(cut, &parked);
-        if (planes > PACKED_MAX_PLANES || (n > 1 && (double)planes * rows * KV * (p->head_dim * 4 + 8) > 1e9)) break;
+        if (planes > PACKED_MAX_PLANES || n_items > most_items || (n > 1 && (double)planes * rows * KV * (p->head_dim * 4 + 8) > 1e9)) break;
         const double rest = planes ? (packed_by_arrival(p) ? 1.0 + 0.3 * planes : C.join) + parked * KV * C.plane_row : 0.0;
         if (rest >= least) break;
         // a plan with partial results has to be a good deal faster: whole launches run at their power limit, where idle places at the end
@@ -1079,8 +1096,7 @@ static double packed_lay_out(const pf_packed *p, const PackedCosts &C, bool take
   return least;
 }
 
-constexpr long long PACKED_MAX_ITEMS = (1 << 23) - 1;             // a launch has fewer than 2^32 threads, an item up to 512
-static int packed_make(const pf_packed *p, PackedPlan &plan) {
+static void packed_make(const pf_packed *p, PackedPlan &plan) {
   PackedLayout L;
   double least = 1e300;
   for (int wide = 0; wide < (p->head_dim == 128 && !packed_by_arrival(p) ? 2 : 1); ++wide)
@@ -1094,9 +1110,6 @@ static int packed_make(const pf_packed *p, PackedPlan &plan) {
       }
     }
   plan.planes = L.planes;
-  long long n_items = 0;
-  for (const int n : L.cuts) n_items += (long long)n * p->n_kv_heads;
-  if (n_items > PACKED_MAX_ITEMS) return PF_ERR_UNSUPPORTED;
   struct Loaded {
     PackedItem item;
     int load;
@@ -1128,7 +1141,6 @@ static int packed_make(const pf_packed *p, PackedPlan &plan) {
     for (size_t d = 0; d < PF_NUM_XCD; ++d)
       for (size_t i = a + (d + PF_NUM_XCD - a % PF_NUM_XCD) % PF_NUM_XCD; i < b; i += PF_NUM_XCD) plan.items[i] = items[from++].item;
   }
-  return PF_OK;
 }
 
 // What a plan is for: with anything else its items would point outside the tensors.
@@ -1160,17 +1172,9 @@ static int packed_guard(F &&f) {
 }
 
 extern "C" size_t pf_packed_work_bytes(const pf_packed *packed) {
-  size_t n = 0;
-  packed_guard([&]() {
-    const int rc = packed_check(packed);
-    if (rc != PF_OK) return rc;
-    PackedPlan plan;
-    const int made = packed_make(packed, plan);
-    if (made != PF_OK) return made;
-    n = packed_plan_bytes(plan.items.size(), packed->n_kv_heads);
-    return PF_OK;
-  });
-  return n;
+  if (packed_check(packed) != PF_OK) return 0;
+  const long long items = packed_most_items(packed);
+  return items > PACKED_MAX_ITEMS ? 0 : packed_plan_bytes((size_t)items, packed->n_kv_heads);
 }
 
 extern "C" int pf_packed_plan(pf_packed *packed, void *stream) {
@@ -1178,10 +1182,12 @@ extern "C" int pf_packed_plan(pf_packed *packed, void *stream) {
     const int rc = packed_check(packed);
     if (rc != PF_OK) return rc;
     if (!packed->work || ((uintptr_t)packed->work & 31u)) return (int)PF_ERR_INVALID_ARG;
+    const size_t need = pf_packed_work_bytes(packed);
+    if (need == 0) return (int)PF_ERR_UNSUPPORTED;
+    if (packed->work_bytes < need) return (int)PF_ERR_CAPACITY;
     PackedPlan plan;
-    const int made = packed_make(packed, plan);
-    if (made != PF_OK) return made;
-    if (packed->work_bytes < packed_plan_bytes(plan.items.size(), packed->n_kv_heads)) return (int)PF_ERR_CAPACITY;
+    packed_make(packed, plan);
+    if (plan.items.size() > (size_t)packed_most_items(packed)) return (int)PF_ERR_UNSUPPORTED;
     PackedItem *to = (PackedItem *)packed->work;
     for (size_t i = 0; i < plan.items.size(); i += PACKED_UPLOAD) {
       PackedUpload U;
