@@ -41,7 +41,7 @@ struct __attribute__((aligned(32))) PackedItem {
 };
 constexpr int PACKED_MAX_PLANES = 256;
 constexpr int PACKED_JOIN_BATCHES = PACKED_MAX_PLANES / 64;
-constexpr int PACKED_FEW_PLANES = 4;
+constexpr int PACKED_FEW_PLANES = 4;                              // joined by groups of lanes (118 and 50 us where a wave for every row takes 126 and 55)
 constexpr int PACKED_PREFIX_BIT = 12;
 PF_HD int packed_head(const PackedItem &it) { return it.head & 0xfff; }
 PF_HD bool packed_has_prefix(const PackedItem &it) { return (it.head >> PACKED_PREFIX_BIT) & 1; }
@@ -63,8 +63,13 @@ __global__ void pf_packed_upload_kernel(PackedUpload U, int n, PackedItem *to, i
 constexpr int PACKED_WAVES = 4;
 constexpr int PACKED_ROWS = 32 * PACKED_WAVES;                    // rows of a full item
 constexpr int PACKED_WIDE_ROWS = 256;                             // ... and of a wide one (pf_packed_wide.h)
-constexpr int PACKED_ARRIVE_ROWS = 32;                            // rows that a head may have for its last workgroup to join them
-constexpr int PACKED_THIN_ROWS = 32;                              // lines of at most so many rows are thin items
+// Rows that a head may have for its last workgroup to join them.  It saves the host the second launch (8 tokens behind 2048: 12.0 us a call, 14.9
+// with it) and costs the GPU the last arrival and round trips to memory one after the other: 12 heads behind 4096 keys, replayed from a graph, take
+// 10.7, 11.9, 15.4 and 31.6 us for 1, 8, 16 and 32 rows, with a second launch 9.6, 10.7, 13.8 and 17.3.
+constexpr int PACKED_ARRIVE_ROWS = 8;
+// Lines of at most so many rows are thin items: 16 sequences of 8 to 32 rows against 2000 keys of 8 heads 24 to 25 us, as full items 28 to 29;
+// head_dim 64: 15 and 18 (of 2 rows: 19 and 18).
+constexpr int PACKED_THIN_ROWS = 32;
 
 struct PackedParams {
   const __bf16 *q, *k, *v, *k_prefix, *v_prefix;

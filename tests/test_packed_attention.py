@@ -464,9 +464,10 @@ def test_streams_graphs_and_two_batches_at_once():
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("D", [64, 128])
-@pytest.mark.parametrize("seqs,H,KV,P,keys", [(1, 8, 8, 0, 5000), (4, 8, 1, 3000, 70), (8, 4, 4, 700, 300), (32, 3, 3, 2000, 9), (33, 3, 3, 2000, 9)])
+@pytest.mark.parametrize("seqs,H,KV,P,keys", [(1, 8, 8, 0, 5000), (4, 8, 1, 3000, 70), (8, 4, 4, 700, 300), (32, 3, 3, 2000, 9), (33, 3, 3, 2000, 9),
+                                                 (2, 8, 2, 2500, 64), (9, 2, 2, 2500, 64)])
 def test_few_rows_split_over_many_workgroups(seqs, H, KV, P, keys, D):
-    """Up to 32 rows a head are joined by the head's last workgroup, more by a second launch: launch after launch and replay after replay
+    """Up to 8 rows a head are joined by the head's last workgroup, more by a second launch: launch after launch and replay after replay
     with the same bits, the plan's counters back at zero."""
     cu_q, cu_k = _cu([1] * seqs), _cu([keys + 3 * i for i in range(seqs)])
     q, k, v, kp, vp = _tensors(H, KV, D, cu_q[-1], cu_k[-1], P, 71, True)
