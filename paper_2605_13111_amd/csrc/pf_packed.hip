@@ -13,6 +13,14 @@
 // park unnormalised partial results (O, m, l) in fp32, one plane per item, row by row, and they are joined plane by plane in a fixed
 // order: by a second kernel, or, where a head has a few rows only, by the head's last workgroup to finish (no spinning).
 //
+// Three kinds of items.  Full: 128 rows, four waves, two workgroups per compute unit (four at head_dim 64) that fill each other's gaps.  Wide
+// (pf_packed_wide.h): 256 rows, eight waves that alternate between matrix and vector work, one workgroup per compute unit; a whole batch is
+// laid out with one or the other, whichever the planner finds faster (one head_dim-128 prompt of 16 heads: 1200 tokens 24 us either way,
+// 4800 tokens 109 full and 101 wide, 9600 tokens 340 and 319).  Thin: at most 32 rows, among the full ones.
+// Bound: prompts by the matrix pipe and the power it may draw (14040 tokens of 12 heads 1210 TFLOP/s, where a plain product of 8192^3 reaches
+// 1214; head_dim 64 by the vector ALU too: 966), single tokens by HBM (64 answers behind 16384 tokens: 4.6 TB/s, a plain copy 4.9), short
+// launches by what an item costs whatever its length: some 3 us to its first tile and 1.5 for its results.
+//
 // Scores, softmax and value products as in the ragged-cache kernels: S^T = K Q^T and O^T += V^T P^T on 32x32x16 bf16 MFMAs with fp32
 // accumulation, one query row per lane; weights are rounded to bf16 for the second product (2^-8 relative at most each, the sum is
 // taken in fp32 before that rounding).

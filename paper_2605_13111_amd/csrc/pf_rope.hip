@@ -10,6 +10,7 @@
 // Bound: HBM, every row is read and written once.  A wave takes one token (or some of its heads, where tokens are few): its lanes work
 // the token's cosines and sines out once, one pair each, and all heads of the token share them; a row is D / 8 lanes wide, and a
 // lane holds whole pairs in either layout (eight neighbouring channels, or four of each half), so that nothing crosses lanes but the sum of squares.
+// 88920 tokens of 24 heads of 128: 190 us, 5.7 TB/s read and written (a plain copy: 4.9).
 #include <math.h>
 #include "pf_internal.h"
 
@@ -18,8 +19,10 @@ typedef __attribute__((ext_vector_type(4))) float rope_f4;
 
 constexpr int ROPE_THREADS = 256;
 constexpr int ROPE_WAVES = ROPE_THREADS / 64;
-constexpr int ROPE_MIN_WAVES = 8192;                              // 32 per compute unit
-constexpr int ROPE_AHEAD = 3;                                     // groups of rows in flight per wave
+// A token's heads are dealt out to several waves until there are so many, 32 per compute unit: 4680 tokens of 24 heads 12.8 us (with 16384 15.3, with
+// 32768 21.0: the angles are worked out once per wave)
+constexpr int ROPE_MIN_WAVES = 8192;
+constexpr int ROPE_AHEAD = 3;                                     // groups of rows in flight per wave (2: 199.6 us for 88920 tokens, 3: 190, 4: 213)
 
 struct RopeParams {
   const __bf16 *x[2], *weight[2];                                 // queries, keys
