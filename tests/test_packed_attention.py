@@ -330,6 +330,31 @@ def test_masked_keys_do_not_count_in_wide_items(bad):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("D,n", [(64, 300), (128, 300), (128, 1200)])
+def test_a_query_that_is_not_a_number_stays_alone(D, n, bad):
+    """The other rows of its tile, and of the waves beside it, have the bits that they had."""
+    KV, cu = (_wide([n], [n], 1, 1) if n == 1200 else 3), _cu([n])
+    q, k, v, kp, vp = _tensors(KV, KV, D, n, n, 0 if n == 1200 else 70, 37, True)
+    out = _run_bits(cu, q, k, v, kp, vp)
+    q[1, 133] = bad
+    got = _run_bits(cu, q, k, v, kp, vp)
+    same = got == out
+    assert torch.isnan(got[1, 133].view(torch.bfloat16)).all()
+    same[1, 133] = True
+    assert same.all()
+
+
+def _run_bits(cu, q, k, v, kp, vp):
+    packed = B.Packed(cu, cu, q.shape[0], k.shape[0], q.shape[2], block=1, prefix_tokens=0 if kp is None else kp.shape[1], device=DEV)
+    B.pf_packed_plan(packed)
+    ws, out = torch.zeros(B.pf_packed_workspace_bytes(packed), dtype=torch.uint8, device=DEV), torch.empty(q.shape, dtype=torch.bfloat16, device=DEV)
+    B.pf_packed_attn_fwd(packed, q, k, v, out, ws, kp, vp)
+    torch.cuda.synchronize()
+    return out.view(torch.int16)
+
+
+@pytest.mark.gpu
 def test_rows_behind_the_last_sequence_of_wide_items():
     lq = [1100, 77]
     KV, cu, n = _wide(lq, lq, 2, 1), _cu(lq), 1177
