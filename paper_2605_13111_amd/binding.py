@@ -424,7 +424,9 @@ def pf_qk_norm_rope(rope, positions, q, q_out, k=None, k_out=None, q_weight=None
 
 class Packed:
     """A batch of packed sequences: its lengths (``cu_q``, ``cu_k``: token offsets, n_seqs + 1 each, on the host), heads and mask, the
-    plan's buffer and the ``pf_packed`` struct.  block: 0 = no mask, 1 = causal, n = causal by blocks of n tokens."""
+    plan's buffer and the ``pf_packed`` struct.  block: 0 = no mask, 1 = causal, n = causal by blocks of n tokens.  The offsets may be
+    written over (``cu_k[i] = ...``, as sequences grow); the batch is refused then until it is planned again.  The plan's buffer is
+    good for any keys, and for no more queries."""
 
     def __init__(self, cu_q, cu_k, n_heads, n_kv_heads, head_dim, block=1, prefix_tokens=0, device="cuda:0"):
         cu_q, cu_k = [int(x) for x in cu_q], [int(x) for x in cu_k]
@@ -464,10 +466,11 @@ def pf_packed_attn_fwd(packed, q, k, v, out, workspace, k_prefix=None, v_prefix=
     """q, out: bf16 views of logical shape [n_heads, total_q, head_dim]; k, v: [n_kv_heads, total_k, head_dim]; k_prefix, v_prefix:
     [n_kv_heads, prefix_tokens, head_dim] -- e.g. [tokens, heads, head_dim] tensors seen heads first; no copy is made.  k and v share a
     stride pattern, and so do the prefix's.  workspace: uint8 tensor.  All on the current device, which is the plan's."""
-    H, KV, tq, D, dev = packed.n_heads, packed.n_kv_heads, packed.total_q, packed.D, _current_device()
+    c, dev = packed.c, _current_device()                          # what the plan is for: the lengths may have been written over in place
+    H, KV, tq, D, P = c.n_heads, c.n_kv_heads, c.total_q, c.head_dim, c.prefix_tokens
     kp = vp = pl = None
-    if packed.prefix_tokens:
-        pl = _packed_layout(KV, packed.prefix_tokens, D, dev, k_prefix, v_prefix)
+    if P:
+        pl = _packed_layout(KV, P, D, dev, k_prefix, v_prefix)
         kp, vp = k_prefix.data_ptr(), v_prefix.data_ptr()
     else:
         assert k_prefix is None and v_prefix is None
@@ -476,8 +479,8 @@ def pf_packed_attn_fwd(packed, q, k, v, out, workspace, k_prefix=None, v_prefix=
         assert workspace.get_device() == dev and workspace.is_contiguous()
         ws, ws_bytes = workspace.data_ptr(), workspace.nbytes
     assert packed.work.get_device() == dev
-    rc = (_lib or lib()).pf_packed_attn_fwd(ctypes.byref(packed.c), q.data_ptr(), _packed_layout(H, tq, D, dev, q), k.data_ptr(), v.data_ptr(),
-                                            _packed_layout(KV, packed.total_k, D, dev, k, v), kp, vp, pl, out.data_ptr(),
+    rc = (_lib or lib()).pf_packed_attn_fwd(ctypes.byref(c), q.data_ptr(), _packed_layout(H, tq, D, dev, q), k.data_ptr(), v.data_ptr(),
+                                            _packed_layout(KV, c.total_k, D, dev, k, v), kp, vp, pl, out.data_ptr(),
                                             _packed_layout(H, tq, D, dev, out), softmax_scale, ws, ws_bytes, _raw_stream(dev) if stream is None else stream)
     if rc:
         raise PfError(rc, "pf_packed_attn_fwd")

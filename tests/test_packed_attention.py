@@ -412,6 +412,15 @@ def test_lengths_that_change_need_a_plan():
     B.pf_packed_attn_fwd(packed, q, k, v, out, ws)
     want, tol = _definition(q, k, v, [0, 20, 100], [0, 20, 100], 1)
     assert ((out.double() - want).abs() <= tol).all()
+    packed.cu_k[2] = 103                                          # three keys more than the tensors have
+    B.pf_packed_plan(packed)
+    with pytest.raises(AssertionError):
+        B.pf_packed_attn_fwd(packed, q, k, v, out, ws)
+    k, v = (torch.cat([t, t[:, :3]], 1) for t in (k, v))
+    assert B.pf_packed_workspace_bytes(packed) <= ws.numel()
+    B.pf_packed_attn_fwd(packed, q, k, v, out, ws)
+    want, tol = _definition(q, k, v, [0, 20, 100], [0, 20, 103], 1)
+    assert ((out.double() - want).abs() <= tol).all()
 
 
 @pytest.mark.gpu
