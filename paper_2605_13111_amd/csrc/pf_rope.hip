@@ -22,6 +22,7 @@ constexpr int ROPE_WAVES = ROPE_THREADS / 64;
 // A token's heads are dealt out to several waves until there are so many, 32 per compute unit: 4680 tokens of 24 heads 12.8 us (with 16384 15.3, with
 // 32768 21.0: the angles are worked out once per wave)
 constexpr int ROPE_MIN_WAVES = 8192;
+constexpr int ROPE_MAX_TOKENS = ((1 << 24) - 1) * ROPE_WAVES;      // a launch has fewer than 2^32 threads
 constexpr int ROPE_AHEAD = 3;                                     // groups of rows in flight per wave (2: 199.6 us for 88920 tokens, 3: 190, 4: 213)
 
 struct RopeParams {
@@ -222,7 +223,7 @@ static int rope_rows_ok(const pf_rope_rows *t, int n_tokens, int head_dim) {
 
 extern "C" int pf_qk_norm_rope(const pf_rope *rope, int n_tokens, const int32_t *positions, const pf_rope_rows *q, const pf_rope_rows *k,
                                float eps, void *stream) {
-  if (!rope || !q || !k || n_tokens < 0 || n_tokens >= (1 << 26)) return PF_ERR_INVALID_ARG;
+  if (!rope || !q || !k || n_tokens < 0 || n_tokens > ROPE_MAX_TOKENS) return PF_ERR_INVALID_ARG;
   const int D = rope->head_dim;
   if (D != 64 && D != 128) return PF_ERR_UNSUPPORTED;
   if (rope->rot_dim < 0 || rope->rot_dim > D || rope->rot_dim % 8 || rope->n_axes < 1 || rope->n_axes > 3) return PF_ERR_INVALID_ARG;

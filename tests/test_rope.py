@@ -105,6 +105,15 @@ def test_calls_refused_without_a_device():
     assert call(r=odd) == B.PF_ERR_UNSUPPORTED
 
 
+def test_the_most_tokens_of_a_call():
+    """A launch has fewer than 2^32 threads: four tokens to a workgroup of 256, fewer than 2^24 workgroups.  The refusal comes before anything
+    is enqueued, so fake addresses do."""
+    L, rope = B.lib(), B.make_rope(64)
+    one = B.pf_rope_rows(0x10000, 0x10000, 0, 1, 0, B.pf_chunk_layout(64, 64 << 26), B.pf_chunk_layout(64, 64 << 26))
+    for n in ((1 << 26) - 3, (1 << 26) - 2, (1 << 26) - 1):
+        assert L.pf_qk_norm_rope(ctypes.byref(rope), n, 0x1000, ctypes.byref(one), ctypes.byref(B.pf_rope_rows()), 1e-6, None) == B.PF_ERR_INVALID_ARG
+
+
 # ---- results ----------------------------------------------------------------------------------------------------------
 
 def _formula(x, w, positions, rope, eps):
