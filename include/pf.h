@@ -357,7 +357,8 @@ typedef struct pf_rope_rows {
  * and pf_cache_append_strided take.
  *   positions  dev int32 [n_axes][n_tokens], any values; may be NULL when rot_dim is 0
  *   eps        > 0; 0 = no norm (weights must be NULL then)
- * q and k must not be NULL; one of them may have n_heads = 0.  n_tokens = 0 does nothing; at most 2^26 - 4.
+ * q and k must not be NULL; one of them may have n_heads = 0.  n_tokens = 0 does nothing (tensors and positions may be
+ * NULL then); at most 2^26 - 4.
  */
 int pf_qk_norm_rope(const pf_rope *rope, int n_tokens, const int32_t *positions, const pf_rope_rows *q,
                     const pf_rope_rows *k, float eps, void *stream);

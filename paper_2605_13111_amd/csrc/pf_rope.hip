@@ -214,7 +214,7 @@ extern "C" int pf_rope_init(pf_rope *rope, int head_dim, int rot_dim, int interl
 static int rope_rows_ok(const pf_rope_rows *t, int n_tokens, int head_dim) {
   if (t->n_heads < 0 || t->n_heads > PF_MAX_HEADS || t->reserved) return PF_ERR_INVALID_ARG;
   if (t->n_heads == 0) return t->x || t->out || t->weight ? PF_ERR_INVALID_ARG : PF_OK;
-  if (!t->x || !t->out) return PF_ERR_INVALID_ARG;
+  if (n_tokens > 0 && (!t->x || !t->out)) return PF_ERR_INVALID_ARG;
   if ((((uintptr_t)t->x) | ((uintptr_t)t->out) | ((uintptr_t)t->weight)) & 15u) return PF_ERR_INVALID_ARG;
   for (const pf_chunk_layout *l : {&t->x_layout, &t->out_layout})
     if ((l->token_stride || l->head_stride) && !pf_chunk_layout_ok(l, t->n_heads, n_tokens, head_dim)) return PF_ERR_INVALID_ARG;
@@ -240,7 +240,7 @@ extern "C" int pf_qk_norm_rope(const pf_rope *rope, int n_tokens, const int32_t 
     const int rc = rope_rows_ok(t, n_tokens, D);
     if (rc != PF_OK) return rc;
   }
-  if (rope->rot_dim > 0 && (!positions || ((uintptr_t)positions & 3u))) return PF_ERR_INVALID_ARG;
+  if (rope->rot_dim > 0 && ((n_tokens > 0 && !positions) || ((uintptr_t)positions & 3u))) return PF_ERR_INVALID_ARG;
   if (n_tokens == 0) return PF_OK;
   RopeParams P = {};
   const pf_rope_rows *t[2] = {q, k};

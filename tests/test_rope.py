@@ -114,6 +114,23 @@ def test_the_most_tokens_of_a_call():
         assert L.pf_qk_norm_rope(ctypes.byref(rope), n, 0x1000, ctypes.byref(one), ctypes.byref(B.pf_rope_rows()), 1e-6, None) == B.PF_ERR_INVALID_ARG
 
 
+def test_no_tokens_need_no_memory():
+    """Tensors without a token have no address; a call on them does nothing.  What is wrong without them is refused all the same."""
+    L, rope, D = B.lib(), B.make_rope(128), 128
+
+    def call(q, k, p=0, n=0):
+        return L.pf_qk_norm_rope(ctypes.byref(rope), n, p, q, k, 1e-6, None)
+
+    x = torch.empty((0, 4, D), dtype=torch.bfloat16).transpose(0, 1)
+    rows = B._rope_rows(D, 0, x.get_device(), x, torch.empty_like(x), None)
+    assert call(rows, rows) == B.PF_OK
+    packed = B.pf_rope_rows(0, 0, 0, 4, 0, B.pf_chunk_layout(0, 0), B.pf_chunk_layout(0, 0))
+    assert call(ctypes.byref(packed), ctypes.byref(B.pf_rope_rows())) == B.PF_OK
+    assert call(rows, rows, n=1) == B.PF_ERR_INVALID_ARG and call(rows, rows, p=0x1000, n=1) == B.PF_ERR_INVALID_ARG
+    packed.x = 0x1008
+    assert call(ctypes.byref(packed), rows) == B.PF_ERR_INVALID_ARG
+
+
 # ---- results ----------------------------------------------------------------------------------------------------------
 
 def _formula(x, w, positions, rope, eps):
