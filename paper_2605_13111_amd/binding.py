@@ -400,6 +400,7 @@ def _rope_rows(D, n_tokens, dev, x, out, weight):
     oh, ot, o1 = out.stride()
     assert x.dtype is _BF16 and out.dtype is _BF16 and out.shape == shape and tokens == n_tokens and d == D and x1 == 1 and o1 == 1
     assert x.get_device() == dev and out.get_device() == dev
+    assert (xt or xh) and (ot or oh)                              # both strides 0 would stand for a packed tensor
     w = 0
     if weight is not None:
         assert weight.dtype is _BF16 and weight.shape == (D,) and weight.stride(0) == 1 and weight.get_device() == dev

@@ -131,6 +131,20 @@ def test_no_tokens_need_no_memory():
     assert call(ctypes.byref(packed), rows) == B.PF_ERR_INVALID_ARG
 
 
+@pytest.mark.parametrize("which", ["x", "out"])
+def test_views_that_repeat_one_row_are_refused(which):
+    """A row expanded over heads and tokens has strides of zero, which the library's structs take for packed tensors."""
+    D, dev = 64, torch.empty(0).get_device()
+    good, bad = torch.zeros((3, 5, D), dtype=torch.bfloat16), torch.zeros(D, dtype=torch.bfloat16).expand(3, 5, D)
+    B._rope_rows(D, 5, dev, good, good, None)
+    with pytest.raises(AssertionError):
+        B._rope_rows(D, 5, dev, bad if which == "x" else good, bad if which == "out" else good, None)
+    L, rope = B.lib(), B.make_rope(D)
+    for strided in (good[:1].expand(3, 5, D), good[:, :1].expand(3, 5, D)):   # one of the strides zero: refused by the library
+        rows = B._rope_rows(D, 5, dev, *((strided, good) if which == "x" else (good, strided)), None)
+        assert L.pf_qk_norm_rope(ctypes.byref(rope), 5, 0x1000, rows, ctypes.byref(B.pf_rope_rows()), 1e-6, None) == B.PF_ERR_INVALID_ARG
+
+
 # ---- results ----------------------------------------------------------------------------------------------------------
 
 def _formula(x, w, positions, rope, eps):
