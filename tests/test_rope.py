@@ -294,3 +294,18 @@ def test_another_stream_and_a_captured_graph():
         assert torch.equal(go, want)
         if seed == 1:
             _check(o, q, None, positions - 1, rope, 1e-6)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("D,rot,interleaved", [(128, 64, False), (128, 8, True), (64, 0, False), (64, 32, True), (64, 8, False)])
+def test_channels_that_are_not_turned_keep_their_bits(D, rot, interleaved):
+    """Without a norm the channels behind rot_dim come out as they went in, zeros' signs among them, whatever stands beside them."""
+    rope = B.make_rope(D, rot, interleaved=interleaved, magnitude=1.5)
+    q = synth.randn_bf16((3, 6, D), 4, device=DEV)
+    q[0, :, rot::2], q[1, :, rot + 1::3], q[2, :, rot:] = float("inf"), float("nan"), -0.0
+    q[2, :, rot + 3::4] = -1.0
+    o = torch.zeros_like(q)
+    B.pf_qk_norm_rope(rope, torch.arange(6, dtype=torch.int32, device=DEV)[None], q, o)
+    torch.cuda.synchronize()
+    a, b = (t[..., rot:].contiguous().view(torch.int16) for t in (q, o))
+    assert torch.equal(a, b)
