@@ -392,6 +392,7 @@ typedef struct pf_packed {
   void *work;                     /* dev, >= pf_packed_work_bytes, 32-byte aligned */
   size_t work_bytes;
   uint64_t planned_for;           /* [lib] checksum of the lengths, heads, block and prefix that the plan is for, and of the plan's own sizes */
+  const void *planned_in;         /* [lib] `work` at that time */
 } pf_packed;
 
 /* Bytes of pf_packed.work that pf_packed_plan needs: room for any plan of these heads and query lengths (it does not depend on the
@@ -401,7 +402,7 @@ size_t pf_packed_work_bytes(const pf_packed *packed);
 
 /* Plan the batch: what pf_packed_attn_fwd does for these lengths, heads and block, for any number of calls (the layers of a
  * model).  Writes `work` on the stream (captured into a graph, a replay writes the same plan again).  A change of lengths, heads,
- * head_dim, block or prefix needs a plan of its own: until then the calls below refuse the batch.
+ * head_dim, block or prefix, and another `work`, needs a plan of its own: until then the calls below refuse the batch.
  * PF_ERR_CAPACITY if work_bytes is too small; PF_ERR_UNSUPPORTED where that is 0 for its work items. */
 int pf_packed_plan(pf_packed *packed, void *stream);
 

@@ -1217,6 +1217,7 @@ extern "C" int pf_packed_plan(pf_packed *packed, void *stream) {
     packed->total_q = packed->cu_q[packed->n_seqs];
     packed->total_k = packed->cu_k[packed->n_seqs];
     packed->planned_for = packed_checksum(packed);
+    packed->planned_in = packed->work;
     return (int)PF_OK;
   });
 }
@@ -1248,6 +1249,7 @@ extern "C" int pf_packed_attn_fwd(const pf_packed *packed, const void *q, const 
   const size_t need = packed_part_bytes(packed, packed->n_planes);
   if (need > 0 && (!workspace || workspace_bytes < need)) return PF_ERR_INVALID_ARG;
   if (tq == 0) return PF_OK;
+  if (packed->planned_in != packed->work) return PF_ERR_INVALID_ARG;   // the plan stands in another buffer
   PackedParams P = {};
   P.q = (const __bf16 *)q;
   P.k = (const __bf16 *)k;

@@ -119,6 +119,25 @@ def test_calls_refused_without_a_device():
     assert call(s, kp=fake, vp=fake, pl=(128, 128), ws=0x20000, ws_bytes=need) == bad
 
 
+def test_a_buffer_that_was_not_planned_in_is_refused():
+    """The plan stands in `work`: another buffer in its place, aligned and large enough, holds none.  Everything else is refused where it
+    does stand there, too."""
+    L, fake = B.lib(), 0x10000
+
+    def call(work=0x1000, q=fake, k=fake, v=fake, out=fake, kp=0, ql=(512, 128), kl=(512, 128), ol=(512, 128), scale=0.0, ws=0, ws_bytes=0, planes=0):
+        s = _struct(kv=4)
+        s.n_items, s.n_planes, s.total_q, s.total_k = 4, planes, 9, 9
+        s.planned_for, s.planned_in = _checksum(s), 0x1000
+        s.work = work
+        ql, kl, ol = (ctypes.byref(B.pf_chunk_layout(*x)) for x in (ql, kl, ol))
+        return L.pf_packed_attn_fwd(ctypes.byref(s), q, ql, k, v, kl, kp, None, None, out, ol, scale, ws, ws_bytes, None)
+
+    for kw in (dict(work=0x2000), dict(q=0), dict(k=0), dict(v=0), dict(out=0), dict(q=fake + 8), dict(k=fake + 2), dict(out=fake + 8), dict(kp=fake), dict(ql=(512, 127)),
+               dict(ql=(256, 128)), dict(ol=(384, 128)), dict(kl=(128, 128)), dict(ws=0x10008), dict(scale=-1.0), dict(scale=float("nan")), dict(planes=2),
+               dict(planes=2, ws=0x20000, ws_bytes=2 * 9 * 4 * (128 * 4 + 8) - 1)):
+        assert call(**kw) == B.PF_ERR_INVALID_ARG, kw
+
+
 def test_batches_of_too_many_items_are_refused():
     """8 heads of 2^20 sequences: a launch of 2^23 workgroups would have too many threads."""
     n = 1 << 20
@@ -421,6 +440,26 @@ def test_lengths_that_change_need_a_plan():
     B.pf_packed_attn_fwd(packed, q, k, v, out, ws)
     want, tol = _definition(q, k, v, [0, 20, 100], [0, 20, 103], 1)
     assert ((out.double() - want).abs() <= tol).all()
+
+
+@pytest.mark.gpu
+def test_another_buffer_needs_a_plan():
+    cu = _cu([70, 30])
+    packed = B.Packed(cu, cu, 4, 2, 64, block=1, device=DEV)
+    q, k, v, _, _ = _tensors(4, 2, 64, 100, 100, 0, 29, True)
+    out = torch.empty_like(q)
+    B.pf_packed_plan(packed)
+    ws = torch.empty(B.pf_packed_workspace_bytes(packed), dtype=torch.uint8, device=DEV)
+    B.pf_packed_attn_fwd(packed, q, k, v, out, ws)
+    want = out.clone()
+    packed.work = torch.zeros_like(packed.work)
+    packed.c.work = packed.work.data_ptr()
+    with pytest.raises(B.PfError):
+        B.pf_packed_attn_fwd(packed, q, k, v, out, ws)
+    B.pf_packed_plan(packed)
+    B.pf_packed_attn_fwd(packed, q, k, v, out.zero_(), ws)
+    torch.cuda.synchronize()
+    assert torch.equal(out, want)
 
 
 @pytest.mark.gpu
