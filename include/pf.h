@@ -403,6 +403,9 @@ size_t pf_packed_work_bytes(const pf_packed *packed);
 /* Plan the batch: what pf_packed_attn_fwd does for these lengths, heads and block, for any number of calls (the layers of a
  * model).  Writes `work` on the stream (captured into a graph, a replay writes the same plan again).  A change of lengths, heads,
  * head_dim, block or prefix, and another `work`, needs a plan of its own: until then the calls below refuse the batch.
+ * `work` holds the last plan that was made in it, and no other.  A launch under another one (of another struct that shares the
+ * buffer, of a graph captured before the batch was planned anew, of a plan that is captured and not replayed yet) finds that out on
+ * the device: it writes NaN to every row of `out` and touches nothing else.
  * PF_ERR_CAPACITY if work_bytes is too small; PF_ERR_UNSUPPORTED where that is 0 for its work items. */
 int pf_packed_plan(pf_packed *packed, void *stream);
 

@@ -254,7 +254,10 @@ __device__ __forceinline__ void packed_wide(const PackedItem &it, char *smem, in
 
 __global__ __launch_bounds__(WIDE_WAVES * 64, 2) void pf_packed_wide_kernel(PackedParams) {
   __shared__ __attribute__((aligned(1024))) char smem[(WIDE_KSTAGES + WIDE_VSTAGES) * WIDE_TILE];
-  packed_wide(packed_item(), smem, threadIdx.x);
+  bool there;
+  const PackedItem it = packed_item(there);
+  if (__builtin_expect(!there, 0)) packed_no_plan<128>(threadIdx.x, WIDE_WAVES * 64);
+  else packed_wide(it, smem, threadIdx.x);
 }
 
 #endif  // PF_PACKED_WIDE_H

@@ -462,6 +462,87 @@ def test_another_buffer_needs_a_plan():
     assert torch.equal(out, want)
 
 
+PLANS = {  # lengths of queries, of keys, heads, key heads, head_dim, prefix: full, thin (joined by the last workgroup, or by a second launch), wide
+    "full": ([300, 41], [300, 41], 4, 2, 64, 0), "arrival": ([1] * 4, [900] * 4, 4, 2, 128, 700), "joined": ([1] * 40, [70] * 40, 8, 2, 128, 3000),
+    "wide": ([1200], [1200], 0, 0, 128, 0), "tiny": ([1], [1], 1, 1, 64, 0)}
+
+
+def _planned(name, work=None):
+    lq, lk, H, KV, D, P = PLANS[name]
+    if name == "wide":
+        H = KV = _wide(lq, lk, 1, 1)
+    packed = B.Packed(_cu(lq), _cu(lk), H, KV, D, block=1, prefix_tokens=P, device=DEV)
+    if work is not None:
+        assert packed.c.work_bytes <= work.numel()
+        packed.work = work
+        packed.c.work, packed.c.work_bytes = work.data_ptr(), work.numel()
+    q, k, v, kp, vp = _tensors(H, KV, D, sum(lq), sum(lk), P, 83, True)
+    ws = torch.empty(1 << 27, dtype=torch.uint8, device=DEV)
+
+    def call(out):
+        B.pf_packed_attn_fwd(packed, q, k, v, out, ws, kp, vp)
+    return packed, call, torch.zeros((sum(lq), H, D), dtype=torch.bfloat16, device=DEV).transpose(0, 1)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name", ["full", "arrival", "joined", "wide", "tiny"])
+@pytest.mark.parametrize("other", ["full", "arrival", "wide", "tiny"])
+def test_a_buffer_holds_its_last_plan_only(name, other):
+    """Two batches that share the plan's buffer: a call under the plan that is not there any more, eager or in a graph captured while it was, says so in
+    every row; planned again, the same graph is right again."""
+    packed, call, out = _planned(name)
+    B.pf_packed_plan(packed)
+    assert B.pf_packed_workspace_bytes(packed) <= 1 << 27
+    assert packed.c.kernel == int(name == "wide") and (packed.c.n_planes > 0) == (name in ("arrival", "joined"))
+    call(out)
+    want = out.clone()
+    work = torch.zeros(1 << 22, dtype=torch.uint8, device=DEV)
+    (packed, call, out), (second, call2, out2) = _planned(name, work), _planned(other, work)
+    B.pf_packed_plan(packed)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(out)
+    graph.replay()
+    assert torch.equal(out, want)
+    if other == name:                                             # the same batch: the same plan, whichever struct it was planned for last
+        B.pf_packed_plan(second)
+        graph.replay()
+        assert torch.equal(out, want)
+        call2(out2)
+        assert torch.equal(out2, want)
+        return
+    for _ in range(2):
+        B.pf_packed_plan(second)
+        before = work.clone()
+        call(out.zero_())
+        assert torch.isnan(out).all()
+        out.zero_()
+        graph.replay()
+        assert torch.isnan(out).all() and torch.equal(work, before)
+        call2(out2)
+        assert torch.isfinite(out2).all()
+        B.pf_packed_plan(packed)
+        graph.replay()
+        assert torch.equal(out, want)
+        call(out.zero_())
+        assert torch.equal(out, want)
+
+
+@pytest.mark.gpu
+def test_a_plan_that_is_not_there_yet():
+    """Captured, a plan reaches its buffer with the first replay."""
+    packed, call, out = _planned("joined")
+    packed.work.zero_()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        B.pf_packed_plan(packed)
+    call(out)
+    assert torch.isnan(out).all()
+    graph.replay()
+    call(out)
+    assert torch.isfinite(out).all()
+
+
 @pytest.mark.gpu
 def test_gaps_between_rows_and_heads():
     """q, k and v as slices of one projection, the results as a slice of a wider buffer."""
