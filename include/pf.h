@@ -393,6 +393,8 @@ typedef struct pf_packed {
   size_t work_bytes;
   uint64_t planned_for;           /* [lib] checksum of the lengths, heads, block and prefix that the plan is for, and of the plan's own sizes */
   const void *planned_in;         /* [lib] `work` at that time */
+  int32_t n_unparked;             /* [lib] rows of a key head that have no partial results though others have */
+  int32_t unused;
 } pf_packed;
 
 /* Bytes of pf_packed.work that pf_packed_plan needs: room for any plan of these heads and query lengths (it does not depend on the
@@ -409,8 +411,9 @@ size_t pf_packed_work_bytes(const pf_packed *packed);
  * PF_ERR_CAPACITY if work_bytes is too small; PF_ERR_UNSUPPORTED where that is 0 for its work items. */
 int pf_packed_plan(pf_packed *packed, void *stream);
 
-/* Bytes of workspace that pf_packed_attn_fwd needs under the plan (partial results of rows whose keys are split); 0 on a bad
- * argument or a batch that has no plan, never 0 otherwise.  Host only. */
+/* Bytes of workspace that pf_packed_attn_fwd needs under the plan: partial results of the rows whose keys are split, and of no others.  Up
+ * to 1e9 bytes, or two planes (8 head_dim + 20 bytes a row) of the rows in front of a prefix where those are more.  0 on a bad argument
+ * or a batch that has no plan, never 0 otherwise.  Host only. */
 size_t pf_packed_workspace_bytes(const pf_packed *packed);
 
 /*

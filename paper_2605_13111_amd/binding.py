@@ -72,7 +72,7 @@ class pf_packed(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("n_seqs", "n_heads", "n_kv_heads", "head_dim", "block", "prefix_tokens", "reserved", "n_items", "n_planes",
                                               "total_q", "total_k", "kernel")] + \
                [("cu_q", ctypes.POINTER(ctypes.c_int32)), ("cu_k", ctypes.POINTER(ctypes.c_int32)), ("work", ctypes.c_void_p), ("work_bytes", ctypes.c_size_t),
-                ("planned_for", ctypes.c_uint64), ("planned_in", ctypes.c_void_p)]
+                ("planned_for", ctypes.c_uint64), ("planned_in", ctypes.c_void_p), ("n_unparked", ctypes.c_int32), ("unused", ctypes.c_int32)]
 
 
 _lib = None

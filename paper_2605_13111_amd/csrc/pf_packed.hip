@@ -10,8 +10,9 @@
 // of few rows (single tokens) would each read the prefix for a tile of which they fill little: in front of the prefix they are stacked,
 // neighbours in one line, and each has its own keys as another line.  A work item is a tile of rows against a run of key tiles of its
 // line: the host cuts the work into items and orders them (pf_packed_plan), heaviest first.  Rows whose keys are cut into several items
-// park unnormalised partial results (O, m, l) in fp32, one plane per item, row by row, and they are joined plane by plane in a fixed
-// order: by a second kernel, or, where a head has a few rows only, by the head's last workgroup to finish (no spinning).
+// park unnormalised partial results (O, m, l) in fp32, one plane per item, and they are joined plane by plane in a fixed order: by a second
+// kernel, or, where a head has a few rows only, by the head's last workgroup to finish (no spinning).  Planes hold the rows that park and no
+// others: they are numbered, head by head, and say themselves which row of the result they are.
 //
 // Three kinds of items.  Full: 128 rows, four waves, two workgroups per compute unit (four at head_dim 64) that fill each other's gaps.  Wide
 // (pf_packed_wide.h): 256 rows, eight waves that alternate between matrix and vector work, one workgroup per compute unit; a whole batch is
@@ -38,7 +39,7 @@
 
 // ---- plan ------------------------------------------------------------------------------------------------------------
 
-struct __attribute__((aligned(32))) PackedItem {
+struct PackedItem {
   int32_t q_base;      // first token of the line of rows (queries of one sequence, or of all of them in front of the prefix)
   int32_t row0;        // first row of the tile in that line
   int32_t n_rows;      // rows of the whole line
@@ -46,6 +47,7 @@ struct __attribute__((aligned(32))) PackedItem {
   int32_t n_keys;      // keys of the line behind the prefix
   int32_t kt0, kt1;    // key tiles of this item: the prefix's (if the line has it), then the line's own
   int32_t head;        // key head | the line has the prefix << 12 | (plane + 1) << 13 (0: unsplit) | further planes without an item << 22 | thin << 31
+  int32_t park;        // row r of the line is the key head's parked row park + r (of an item with a plane)
 };
 constexpr int PACKED_MAX_PLANES = 256;
 constexpr int PACKED_JOIN_BATCHES = PACKED_MAX_PLANES / 64;
@@ -65,7 +67,7 @@ struct __attribute__((aligned(32))) PackedHead {
 };
 
 // Items reach the device as kernel arguments: the call neither allocates nor waits, and can be captured.
-constexpr int PACKED_UPLOAD = 120;
+constexpr int PACKED_UPLOAD = 108;                                // kernel arguments end at 4096 bytes
 struct PackedUpload {
   PackedItem item[PACKED_UPLOAD];
 };
@@ -91,12 +93,14 @@ struct PackedParams {
   const __bf16 *q, *k, *v, *k_prefix, *v_prefix;
   __bf16 *out;
   const PackedItem *items;
-  float *part_o;                                                  // [planes][rows][D]
-  float2 *part_ml;                                                // [planes][rows]: reference maximum, sum of weights; a sum of -1 in plane 0: the row is done
+  float *part_o;                                                  // [planes][part_rows][D]
+  float2 *part_ml;                                                // [planes][part_rows]: reference maximum, sum of weights
+  int32_t *part_row;                                              // [part_rows]: token x heads + head
   long long q_tok, q_head, out_tok, out_head, kv_tok, kv_head, pre_tok, pre_head;    // element strides
   int n_rows, n_heads, group, block;                              // n_rows: tokens x heads
   int32_t *arrivals;                                              // [key heads] workgroups of the head that are done; null: a second kernel joins
   int items_per_head;
+  int head_rows, part_rows;                                       // parked rows of a key head, of all
   int planes, prefix_tokens, prefix_tiles;
   unsigned group_mul, group_shift;                                // n / group = (n * group_mul) >> 32 >> group_shift
   float scale_log2;
@@ -124,26 +128,28 @@ __device__ __forceinline__ PackedParams packed_params() {
   PackedParams P = __builtin_bit_cast(PackedParams, words);
   P.q = packed_global(P.q), P.k = packed_global(P.k), P.v = packed_global(P.v), P.k_prefix = packed_global(P.k_prefix);
   P.v_prefix = packed_global(P.v_prefix), P.out = packed_global(P.out), P.items = packed_global(P.items);
-  P.part_o = packed_global(P.part_o), P.part_ml = packed_global(P.part_ml), P.arrivals = packed_global(P.arrivals);
+  P.part_o = packed_global(P.part_o), P.part_ml = packed_global(P.part_ml), P.part_row = packed_global(P.part_row), P.arrivals = packed_global(P.arrivals);
   return P;
 }
 
 // The plan was written before this launch and is constant during it: scalar loads, so that what follows from an item is scalar too.
-typedef const __attribute__((address_space(4))) unsigned long long *packed_words_t;
+typedef const __attribute__((address_space(4))) unsigned *packed_words_t;
 __device__ __forceinline__ bool packed_is_there(const PackedParams &P) {
-  return ((packed_words_t)((const PackedHead *)P.items - 1))[0] == P.planned_for;
+  return *(const __attribute__((address_space(4))) uint64_t *)((const PackedHead *)P.items - 1) == P.planned_for;
 }
 // This workgroup's item; is it one of the call's plan?
 __device__ __forceinline__ PackedItem packed_item(bool &there) {
   struct Words {
-    unsigned long long w[sizeof(PackedItem) / 8];
+    unsigned w[sizeof(PackedItem) / 4];
   } words;
   const PackedParams P = packed_params();
   const packed_words_t from = (packed_words_t)(P.items + blockIdx.x);
 #pragma unroll
-  for (int i = 0; i < (int)(sizeof(PackedItem) / 8); ++i) words.w[i] = from[i];
+  for (int i = 0; i < (int)(sizeof(PackedItem) / 4); ++i) words.w[i] = from[i];
   there = packed_is_there(P);
-  return __builtin_bit_cast(PackedItem, words);
+  PackedItem it = __builtin_bit_cast(PackedItem, words);
+  asm volatile("" : "+v"(it.park));                               // through the loop over the key tiles it would be one scalar too many
+  return it;
 }
 // It is not: the launch says so in every row of the result, and touches nothing else.
 template <int D>
@@ -411,27 +417,27 @@ struct PackedTo {
   float inv;
   bool past_l2;
 };
-// note: this lane also notes the row's maximum and sum, and what the join has to know of the other planes
+// note: this lane also notes the row's maximum and sum, and with plane 0, of which every parked row has one item, which row of the result it is
 template <int D>
 __device__ __forceinline__ PackedTo<D> packed_to(const PackedParams &P, const PackedItem &it, int row, float2 ml, bool note) {
   const int t = packed_div_group(P, row), h = packed_head(it) * P.group + row - t * P.group, plane = packed_plane(it);
-  const long long id = (long long)(it.q_base + t) * P.n_heads + h;
   PackedTo<D> to = {nullptr, nullptr, 1.0f, P.arrivals != nullptr};
-  auto put_ml = [&](int p, float2 x) __attribute__((always_inline)) {
-    float2 *at = P.part_ml + (long long)p * P.n_rows + id;
-    if (to.past_l2) packed_st8(at, x.x, x.y);
-    else *at = x;
-  };
   if (plane >= 0) {
-    to.part = P.part_o + ((long long)plane * P.n_rows + id) * D;
+    const int id = packed_head(it) * P.head_rows + it.park + row;
+    auto put_ml = [&](int p, float2 x) __attribute__((always_inline)) {
+      float2 *at = P.part_ml + (long long)p * P.part_rows + id;
+      if (to.past_l2) packed_st8(at, x.x, x.y);
+      else *at = x;
+    };
+    to.part = P.part_o + ((long long)plane * P.part_rows + id) * D;
     if (note) {
       put_ml(plane, ml);
       for (int i = 1; i <= packed_missing(it); ++i) put_ml(plane + i, make_float2(-3.0e38f, 0.0f));
+      if (plane == 0) __hip_atomic_store(P.part_row + id, (it.q_base + t) * P.n_heads + h, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
   } else {
     to.out = P.out + (it.q_base + t) * P.out_tok + h * P.out_head;
     to.inv = ml.y > 0.0f ? 1.0f / ml.y : ml.y;                    // no key seen: zeros (a sum that is NaN stays NaN)
-    if (P.planes > 0 && note) put_ml(0, make_float2(0.0f, -1.0f));
   }
   return to;
 }
@@ -482,24 +488,18 @@ __device__ __forceinline__ void packed_arrive(const PackedItem &it, int32_t *s_l
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
 #endif
   constexpr int LANES = D / 8, AHEAD = 4;
-  const int n = P.n_rows / P.n_heads * P.group, d0 = tid % LANES * 8;
-  for (int r = tid / LANES; r < n; r += PACKED_WAVES * 64 / LANES) {
-    const int t = packed_div_group(P, r), h = head * P.group + r - t * P.group;
-    const long long id = (long long)t * P.n_heads + h;
+  const int d0 = tid % LANES * 8;
+  for (int r = tid / LANES; r < P.head_rows; r += PACKED_WAVES * 64 / LANES) {
+    const int id = head * P.head_rows + r, row = __hip_atomic_load(P.part_row + id, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     float top = -3.0e38f, sum = 0.0f, acc[8] = {};
-    bool done = false;
     for (int p0 = 0; p0 < P.planes; p0 += AHEAD) {
       float2 ml[AHEAD], x[AHEAD][4];
 #pragma unroll
       for (int i = 0; i < AHEAD; ++i) {                           // (the last plane again once they run out)
-        const long long at = (long long)pf_min(p0 + i, P.planes - 1) * P.n_rows + id;
+        const long long at = (long long)pf_min(p0 + i, P.planes - 1) * P.part_rows + id;
         ml[i] = packed_ld8(P.part_ml + at);
 #pragma unroll
         for (int e = 0; e < 4; ++e) x[i][e] = packed_ld8(P.part_o + at * D + d0 + 2 * e);
-      }
-      if (p0 == 0 && ml[0].y == -1.0f) {                          // written by its only item
-        done = true;
-        break;
       }
       float new_top = top;
 #pragma unroll
@@ -518,12 +518,11 @@ __device__ __forceinline__ void packed_arrive(const PackedItem &it, int32_t *s_l
         for (int e = 0; e < 4; ++e) acc[2 * e] += w * x[i][e].x, acc[2 * e + 1] += w * x[i][e].y;
       }
     }
-    if (done) continue;
     const float inv = sum > 0.0f ? 1.0f / sum : sum;
     bf16x8 w;
 #pragma unroll
     for (int e = 0; e < 8; ++e) w[e] = (__bf16)(acc[e] * inv);
-    *(bf16x8 *)(P.out + t * P.out_tok + h * P.out_head + d0) = w;
+    *(bf16x8 *)(P.out + row / P.n_heads * P.out_tok + row % P.n_heads * P.out_head + d0) = w;
   }
 }
 // A wave's O^T (lane = row l32) as rows of LDS.
@@ -797,19 +796,19 @@ static_assert(PACKED_ARRIVE_ROWS <= PACKED_THIN_ROWS, "full and wide items have 
 #include "pf_packed_wide.h"
 
 
-// Joins the planes of every row: out = sum_p 2^((m_p - M) c) O_p / sum_p 2^((m_p - M) c) l_p.
+// Joins the planes of every parked row: out = sum_p 2^((m_p - M) c) O_p / sum_p 2^((m_p - M) c) l_p.
 //
 // Few planes: D / 8 lanes take a row, eight channels each, plane after plane.
 template <int D>
 __global__ __launch_bounds__(256) void pf_packed_join_few_kernel(PackedParams P) {
   constexpr int LANES = D / 8;
   const int id = blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
-  if (id >= P.n_rows) return;
-  const int d0 = threadIdx.x % LANES * 8;
+  if (id >= P.part_rows) return;
+  const bool there = packed_is_there(P);
+  const int d0 = threadIdx.x % LANES * 8, row = P.part_row[id];
   float2 ml[PACKED_FEW_PLANES];
 #pragma unroll
-  for (int p = 0; p < PACKED_FEW_PLANES; ++p) ml[p] = p < P.planes ? P.part_ml[(long long)p * P.n_rows + id] : make_float2(-3.0e38f, 0.0f);
-  if (ml[0].y == -1.0f || !packed_is_there(P)) return;            // written by its only item
+  for (int p = 0; p < PACKED_FEW_PLANES; ++p) ml[p] = p < P.planes ? P.part_ml[(long long)p * P.part_rows + id] : make_float2(-3.0e38f, 0.0f);
   float top = ml[0].x, sum = 0.0f, acc[8] = {};
 #pragma unroll
   for (int p = 1; p < PACKED_FEW_PLANES; ++p) top = fmaxf(top, ml[p].x);
@@ -818,7 +817,7 @@ __global__ __launch_bounds__(256) void pf_packed_join_few_kernel(PackedParams P)
   for (int p = 0; p < PACKED_FEW_PLANES; ++p) {
     x[p][0] = x[p][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     if (ml[p].y == 0.0f) continue;                                // a plane that saw no key (or has no item) counts nothing
-    const float *o = P.part_o + ((long long)p * P.n_rows + id) * D + d0;
+    const float *o = P.part_o + ((long long)p * P.part_rows + id) * D + d0;
     x[p][0] = *(const f32x4 *)o;
     x[p][1] = *(const f32x4 *)(o + 4);
   }
@@ -830,11 +829,12 @@ __global__ __launch_bounds__(256) void pf_packed_join_few_kernel(PackedParams P)
 #pragma unroll
     for (int e = 0; e < 4; ++e) acc[e] += w * x[p][0][e], acc[e + 4] += w * x[p][1][e];
   }
+  if (!there) return;
   const float inv = sum > 0.0f ? 1.0f / sum : sum;
   bf16x8 r;
 #pragma unroll
   for (int i = 0; i < 8; ++i) r[i] = (__bf16)(acc[i] * inv);
-  *(bf16x8 *)(P.out + id / P.n_heads * P.out_tok + id % P.n_heads * P.out_head + d0) = r;
+  *(bf16x8 *)(P.out + row / P.n_heads * P.out_tok + row % P.n_heads * P.out_head + d0) = r;
 }
 // Many planes: a wave takes a row: its lanes look at a
 // plane's maximum and sum each, then groups of D / 8 lanes (eight channels a lane) add up every 64 / (D / 8)-th plane and the groups'
@@ -845,16 +845,16 @@ __global__ __launch_bounds__(256) void pf_packed_join_kernel(PackedParams P) {
   constexpr int LANES = D / 8, GROUPS = 64 / LANES;
   const int lane = threadIdx.x & 63;
   const int id = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (id >= P.n_rows) return;
-  const int d0 = lane % LANES * 8, grp = lane / LANES;
+  if (id >= P.part_rows) return;
+  const bool there = packed_is_there(P);
+  const int d0 = lane % LANES * 8, grp = lane / LANES, row = P.part_row[id];
   float2 ml[PACKED_JOIN_BATCHES];
   float top = -3.0e38f;
 #pragma unroll
   for (int b = 0; b < PACKED_JOIN_BATCHES; ++b) {
     ml[b] = make_float2(-3.0e38f, 0.0f);
-    if (b * 64 + lane < P.planes) ml[b] = P.part_ml[(long long)(b * 64 + lane) * P.n_rows + id];
+    if (b * 64 + lane < P.planes) ml[b] = P.part_ml[(long long)(b * 64 + lane) * P.part_rows + id];
   }
-  if (__builtin_amdgcn_readfirstlane(__float_as_int(ml[0].y)) == __float_as_int(-1.0f) || !packed_is_there(P)) return;   // written by its only item
 #pragma unroll
   for (int b = 0; b < PACKED_JOIN_BATCHES; ++b) top = fmaxf(top, ml[b].x);
 #pragma unroll
@@ -880,7 +880,7 @@ __global__ __launch_bounds__(256) void pf_packed_join_kernel(PackedParams P) {
         if (p > 63) f[i] = 0.0f;
         x[i][0] = x[i][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         if (f[i] != 0.0f) {
-          const float *o = P.part_o + ((long long)(b * 64 + p) * P.n_rows + id) * D + d0;
+          const float *o = P.part_o + ((long long)(b * 64 + p) * P.part_rows + id) * D + d0;
           x[i][0] = *(const f32x4 *)o;
           x[i][1] = *(const f32x4 *)(o + 4);
         }
@@ -895,12 +895,12 @@ __global__ __launch_bounds__(256) void pf_packed_join_kernel(PackedParams P) {
   for (int step = LANES; step < 64; step *= 2)
 #pragma unroll
     for (int e = 0; e < 8; ++e) acc[e] += packed_lane(acc[e], lane ^ step);
-  if (grp != 0) return;
+  if (grp != 0 || !there) return;
   const float inv = sum > 0.0f ? 1.0f / sum : sum;
   bf16x8 r;
 #pragma unroll
   for (int i = 0; i < 8; ++i) r[i] = (__bf16)(acc[i] * inv);
-  *(bf16x8 *)(P.out + id / P.n_heads * P.out_tok + id % P.n_heads * P.out_head + d0) = r;
+  *(bf16x8 *)(P.out + row / P.n_heads * P.out_tok + row % P.n_heads * P.out_head + d0) = r;
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------
@@ -928,7 +928,7 @@ static int packed_host_limit(const pf_packed *p, int lq, int lk, int query) {
 
 // Plan in pf_packed.work: its head, items, then the heads' arrival counters.
 static size_t packed_plan_bytes(size_t items, int kv_heads) {
-  return sizeof(PackedHead) + items * sizeof(PackedItem) + pf_align_up((size_t)kv_heads * sizeof(int32_t), sizeof(PackedItem));
+  return pf_align_up(sizeof(PackedHead) + items * sizeof(PackedItem) + (size_t)kv_heads * sizeof(int32_t), sizeof(PackedHead));
 }
 static PackedItem *packed_items(const pf_packed *p) { return (PackedItem *)((PackedHead *)p->work + 1); }
 // Room for the plan of any lengths with so many row tiles: theirs and those of stacked lines uncut, and as many items again as several rounds of
@@ -946,7 +946,7 @@ static bool packed_by_arrival(const pf_packed *p) { return (long long)p->cu_q[p-
 
 struct PackedPlan {
   std::vector<PackedItem> items;
-  int planes = 0;
+  int planes = 0, head_rows = 0;   // a key head's rows that park
   bool wide = false;           // items of 256 rows (head_dim 128)
 };
 
@@ -1032,9 +1032,15 @@ static double packed_time(const std::vector<PackedRowTile> &tiles, int heads, co
 struct PackedLayout {
   std::vector<PackedLine> lines;
   std::vector<PackedRowTile> tiles;
-  std::vector<int> cuts, first;  // of every row tile: into how many items its keys are cut, the plane of the first
-  int planes = 0;
+  std::vector<int> cuts, first, park;  // of every row tile: into how many items its keys are cut, the plane of the first, where its line's row 0 parks
+  int planes = 0, head_rows = 0;
 };
+// Partial results: O, and the row's maximum and sum, a plane; and which row it is.  Cuts may bring them to this; two planes of the rows that are
+// stacked, all in front of the prefix and all behind it, are there without any cut.
+constexpr double PACKED_PART_BYTES = 1e9;
+static size_t packed_part_bytes(const pf_packed *p, int planes, long long head_rows) {
+  return planes == 0 ? 0 : (size_t)head_rows * p->n_kv_heads * ((size_t)planes * ((size_t)p->head_dim * 4 + 8) + 4);
+}
 static double packed_lay_out(const pf_packed *p, const PackedCosts &C, bool take_all, PackedLayout &L) {
   const int G = p->n_heads / p->n_kv_heads, KV = p->n_kv_heads, BQ = C.rows;
   const int pre_kt = pf_ceil_div(p->prefix_tokens, PF_BK);
@@ -1061,7 +1067,7 @@ static double packed_lay_out(const pf_packed *p, const PackedCosts &C, bool take
     lines.push_back({p->cu_q[s], r, p->cu_k[s], p->cu_k[s + 1] - p->cu_k[s], pre_kt > 0 && own, stack, false});
   }
   for (PackedLine &l : lines) l.thin = l.n_rows <= C.thin_rows;
-  long long rows = 0, with_prefix = 0;
+  long long with_prefix = 0;
   for (const PackedLine &l : lines)
     if (l.prefix) with_prefix += pf_ceil_div(l.n_rows, BQ);
   // a key tile's time in full tiles: what its bytes take where row tiles that read them are few, if that is more
@@ -1074,7 +1080,6 @@ static double packed_lay_out(const pf_packed *p, const PackedCosts &C, bool take
     for (int r0 = 0; r0 < lines[l].n_rows; r0 += BQ) {
       const int n_kt = packed_line_tiles(p, lines[l], r0, BQ, pre_kt), pre = lines[l].prefix ? pre_kt : 0;
       tiles.push_back({(int)l, r0, n_kt, lines[l].thin, load_of(pre, n_kt - pre, lines[l])});
-      if (lines[l].stack != -2) rows += pf_min(BQ, lines[l].n_rows - r0);
     }
   std::stable_sort(tiles.begin(), tiles.end(), [](const PackedRowTile &a, const PackedRowTile &b) { return a.load > b.load; });
   const int longest = tiles.empty() ? 1 : std::max(1, tiles[0].load);
@@ -1086,17 +1091,18 @@ static double packed_lay_out(const pf_packed *p, const PackedCosts &C, bool take
   auto cuts_of = [&](const PackedCut &cut, size_t i) {
     return lines[tiles[i].line].stack == -2 ? stack_cuts(tiles[i].line, cut.seg) : cut.of((int)i, tiles[i]);
   };
-  long long n_items = 0;
+  long long n_items = 0, head_rows = 0;
   auto planes_of = [&](const PackedCut &cut, double *parked) {
     int most = 0;
     *parked = 0.0;
-    n_items = 0;
+    n_items = head_rows = 0;
     for (size_t i = 0; i < tiles.size(); ++i) {
       const PackedLine &l = lines[tiles[i].line];
       const int n = cuts_of(cut, i), before = l.stack >= 0 ? stack_cuts(l.stack, cut.seg) : 0;
       n_items += (long long)n * KV;
       if (l.stack == -1 && n == 1) continue;
       most = std::max(most, before + n);
+      if (l.stack != -2) head_rows += pf_min(BQ, l.n_rows - tiles[i].row0);
       *parked += (double)n * pf_min(BQ, l.n_rows - tiles[i].row0);
     }
     return most;
@@ -1112,7 +1118,7 @@ static double packed_lay_out(const pf_packed *p, const PackedCosts &C, bool take
       for (int n : {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 40, 48, 64, 80, 96, 120}) {
         const PackedCut cut = {whole, pf_ceil_div(most, n)};
         const int planes = planes_of(cut, &parked);
-        if (planes > PACKED_MAX_PLANES || n_items > most_items || (n > 1 && (double)planes * rows * KV * (p->head_dim * 4 + 8) > 1e9)) break;
+        if (planes > PACKED_MAX_PLANES || n_items > most_items || (n > 1 && (double)packed_part_bytes(p, planes, head_rows) > PACKED_PART_BYTES)) break;
         const double rest = planes ? (packed_by_arrival(p) ? 1.0 + 0.3 * planes : C.join) + parked * KV * C.plane_row : 0.0;
         if (rest >= least) break;
         // a plan with partial results has to be a good deal faster: whole launches run at their power limit, where idle places at the end
@@ -1137,6 +1143,18 @@ static double packed_lay_out(const pf_packed *p, const PackedCosts &C, bool take
     L.cuts.push_back(cuts_of(best, i));
     L.first.push_back(st >= 0 ? stack_cuts(st, best.seg) : 0);
   }
+  // parked rows: those of stacked lines, in which the sequences behind them have theirs, then the other cut tiles'
+  std::vector<int> line_park(lines.size(), 0);
+  for (size_t l = 0; l < lines.size(); ++l) {
+    const PackedLine &x = lines[l];
+    if (x.stack == -2) line_park[l] = L.head_rows, L.head_rows += x.n_rows;
+    if (x.stack >= 0) line_park[l] = line_park[x.stack] + (x.q_base - lines[x.stack].q_base) * G;
+  }
+  for (size_t i = 0; i < tiles.size(); ++i) {
+    const PackedLine &x = lines[tiles[i].line];
+    L.park.push_back(x.stack == -1 ? L.head_rows - tiles[i].row0 : line_park[tiles[i].line]);
+    if (x.stack == -1 && L.cuts[i] > 1) L.head_rows += pf_min(BQ, x.n_rows - tiles[i].row0);
+  }
   return least;
 }
 
@@ -1154,6 +1172,7 @@ static void packed_make(const pf_packed *p, PackedPlan &plan) {
       }
     }
   plan.planes = L.planes;
+  plan.head_rows = L.head_rows;
   struct Loaded {
     PackedItem item;
     int load;
@@ -1165,7 +1184,7 @@ static void packed_make(const pf_packed *p, PackedPlan &plan) {
       const PackedLine &l = L.lines[tile.line];
       const int n = L.cuts[t];
       for (int i = 0; i < n; ++i) {
-        PackedItem it = {l.q_base, tile.row0, l.n_rows, l.k_base, l.n_keys, pf_seg_begin(tile.n_kt, n, i), pf_seg_begin(tile.n_kt, n, i + 1), h};
+        PackedItem it = {l.q_base, tile.row0, l.n_rows, l.k_base, l.n_keys, pf_seg_begin(tile.n_kt, n, i), pf_seg_begin(tile.n_kt, n, i + 1), h, L.park[t]};
         if (l.prefix) it.head |= 1 << PACKED_PREFIX_BIT;
         if (tile.thin) it.head |= (int)(1u << 31);
         if (!(l.stack == -1 && n == 1)) {
@@ -1193,15 +1212,15 @@ static uint64_t packed_checksum(const pf_packed *p) {
   auto add = [&](int32_t x) { h = (h ^ (uint32_t)x) * 1099511628211ull; };
   for (const int32_t x : {p->n_seqs, p->n_heads, p->n_kv_heads, p->head_dim, p->block, p->prefix_tokens, p->n_items, p->n_planes, p->kernel}) add(x);
   for (int s = 1; s <= p->n_seqs; ++s) add(p->cu_q[s]), add(p->cu_k[s]);
+  if (p->n_unparked) add(p->n_unparked);
   return h;
 }
 static bool packed_is_planned(const pf_packed *p) {
   return p->total_q == p->cu_q[p->n_seqs] && p->total_k == p->cu_k[p->n_seqs] && p->planned_for == packed_checksum(p);
 }
 
-static size_t packed_part_bytes(const pf_packed *p, int planes) {
-  return (size_t)planes * p->cu_q[p->n_seqs] * p->n_heads * ((size_t)p->head_dim * 4 + 8);
-}
+// rows of a key head that park under the batch's plan
+static int packed_head_rows(const pf_packed *p) { return p->cu_q[p->n_seqs] * (p->n_heads / p->n_kv_heads) - p->n_unparked; }
 
 // Runs f; memory that the plan needs on the host and does not get is an error, not an exception.
 template <class F>
@@ -1236,6 +1255,8 @@ extern "C" int pf_packed_plan(pf_packed *packed, void *stream) {
     planned.n_items = (int32_t)plan.items.size();
     planned.n_planes = plan.planes;
     planned.kernel = plan.wide ? 1 : 0;
+    planned.n_unparked = 0;
+    if (plan.planes > 0) planned.n_unparked = packed_head_rows(&planned) - plan.head_rows;
     planned.total_q = packed->cu_q[packed->n_seqs];
     planned.total_k = packed->cu_k[packed->n_seqs];
     planned.planned_for = packed_checksum(&planned);
@@ -1258,7 +1279,7 @@ extern "C" int pf_packed_plan(pf_packed *packed, void *stream) {
 
 extern "C" size_t pf_packed_workspace_bytes(const pf_packed *packed) {
   if (packed_check(packed) != PF_OK || !packed_is_planned(packed)) return 0;
-  return pf_align_up(packed_part_bytes(packed, packed->n_planes) + 256, 256);
+  return pf_align_up(packed_part_bytes(packed, packed->n_planes, packed_head_rows(packed)) + 256, 256);
 }
 
 extern "C" int pf_packed_attn_fwd(const pf_packed *packed, const void *q, const pf_chunk_layout *q_layout, const void *k, const void *v,
@@ -1280,7 +1301,7 @@ extern "C" int pf_packed_attn_fwd(const pf_packed *packed, const void *q, const 
       !pf_chunk_layout_ok(kv_layout, packed->n_kv_heads, tk, D) ||
       !pf_chunk_layout_ok(prefix_layout, packed->n_kv_heads, packed->prefix_tokens, D))
     return PF_ERR_INVALID_ARG;
-  const size_t need = packed_part_bytes(packed, packed->n_planes);
+  const size_t need = packed_part_bytes(packed, packed->n_planes, packed_head_rows(packed));
   if (need > 0 && (!workspace || workspace_bytes < need)) return PF_ERR_INVALID_ARG;
   if (tq == 0) return PF_OK;
   if (packed->planned_in != packed->work) return PF_ERR_INVALID_ARG;   // the plan stands in another buffer
@@ -1311,7 +1332,10 @@ extern "C" int pf_packed_attn_fwd(const pf_packed *packed, const void *q, const 
   if (P.planes > 0 && packed_by_arrival(packed)) P.arrivals = (int32_t *)(packed_items(packed) + packed->n_items);
   P.items_per_head = packed->n_items / packed->n_kv_heads;
   P.part_o = (float *)workspace;
-  P.part_ml = (float2 *)((char *)workspace + (size_t)P.planes * P.n_rows * D * 4);
+  P.head_rows = packed_head_rows(packed);
+  P.part_rows = P.head_rows * packed->n_kv_heads;
+  P.part_ml = (float2 *)((char *)workspace + (size_t)P.planes * P.part_rows * D * 4);
+  P.part_row = (int32_t *)(P.part_ml + (size_t)P.planes * P.part_rows);
   P.q_tok = q_layout ? q_layout->token_stride : D;
   P.q_head = q_layout ? q_layout->head_stride : (long long)tq * D;
   P.out_tok = out_layout ? out_layout->token_stride : D;
@@ -1330,7 +1354,7 @@ extern "C" int pf_packed_attn_fwd(const pf_packed *packed, const void *q, const 
   PF_HIP_CHECK(hipGetLastError());
   if (P.planes > 0 && !P.arrivals) {
     const bool few = P.planes <= PACKED_FEW_PLANES;
-    const dim3 rows((unsigned)pf_ceil_div(P.n_rows, few ? 256 / (D / 8) : 4));
+    const dim3 rows((unsigned)pf_ceil_div(P.part_rows, few ? 256 / (D / 8) : 4));
     if (D == 128 && few) hipLaunchKernelGGL((pf_packed_join_few_kernel<128>), rows, block, 0, st, P);
     else if (D == 128) hipLaunchKernelGGL((pf_packed_join_kernel<128>), rows, block, 0, st, P);
     else if (few) hipLaunchKernelGGL((pf_packed_join_few_kernel<64>), rows, block, 0, st, P);

@@ -415,6 +415,30 @@ def test_more_planes_than_a_wave_has_lanes(D):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("lq,lk,H,KV,P,parked", [
+    ([88920, 1], [88920, 1], 24, 12, 2048, 1), ([30000] + [1] * 4, [30000] + [50] * 4, 32, 8, 4096, 4), ([2048] * 7 + [1], [2048] * 7 + [500000], 32, 8, 0, 1),
+    ([2000] * 4 + [1] * 4, [2000] * 4 + [131072] * 4, 32, 8, 0, 4)])
+def test_workspace_holds_the_rows_that_park(lq, lk, H, KV, P, parked):
+    """Prompts whose rows have one item each, beside single tokens whose keys are split: partial results of the tokens only."""
+    D = 128
+    packed = B.Packed(_cu(lq), _cu(lk), H, KV, D, block=1, prefix_tokens=P, device=DEV)
+    B.pf_packed_plan(packed)
+    assert packed.c.n_planes > 1, "the case must park partial results"
+    assert B.pf_packed_workspace_bytes(packed) <= parked * H * (packed.c.n_planes * (D * 4 + 8) + 4) + 512
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("lq,lk,P", [([600] * 3 + [1] * 4, [600] * 3 + [50000] * 4, 0), ([700, 1, 900, 1, 1], [700, 9000, 900, 40, 8000], 500),
+                                     ([1, 300, 1, 0, 2, 129], [7000, 300, 1, 50, 9000, 129], 0), ([1, 1, 2000, 3, 1], [100, 300, 2000, 90, 0], 6000)])
+@pytest.mark.parametrize("H,KV,D", [(8, 2, 128), (8, 2, 64), (3, 3, 128)])
+def test_prompts_beside_single_tokens_of_many_keys(lq, lk, P, H, KV, D):
+    packed = B.Packed(_cu(lq), _cu(lk), H, KV, D, block=1, prefix_tokens=P, device=DEV)
+    B.pf_packed_plan(packed)
+    assert packed.c.n_planes > 1, "the case must park partial results"
+    _case(_cu(lq), _cu(lk), H, KV, D, 1, P, seed=91)
+
+
+@pytest.mark.gpu
 def test_lengths_that_change_need_a_plan():
     """The lengths of a batch written over in place: refused until planned again, right afterwards."""
     packed = B.Packed(_cu([70, 30]), _cu([70, 30]), 4, 2, 64, block=1, device=DEV)
