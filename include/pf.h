@@ -419,7 +419,8 @@ size_t pf_packed_workspace_bytes(const pf_packed *packed);
 /*
  * Attention of the batch:
  *   out[i, h] = sum_j softmax_j(scale * q[i, h] . k[j, h / group]) v[j, h / group]
- * over the prefix and the keys that query i sees (see pf_packed); zeros where it sees none.  bf16 in and out, fp32
+ * over the prefix and the keys that query i sees (see pf_packed); zeros where it sees none, NaN where every score it sees is
+ * minus infinity.  bf16 in and out, fp32
  * accumulation, softmax weights rounded to bf16.  Masked scores never count, whatever K holds there; V has to be finite in
  * every key that a sequence owns.
  *   q, out              dev [n_heads][total_q][head_dim] or by q_layout and out_layout

@@ -243,11 +243,19 @@ __device__ __forceinline__ void packed_copy(const PackedParams &P, const PackedI
 }
 
 // One row's softmax state.  The reference maximum starts below every score; its multiple is kept finite, so that a masked key's weight against
-// it is 0 and not NaN.
+// it is 0 and not NaN.  Where it starts says whether the row sees a key of the item at all: one that does and has no weight in the end saw
+// scores of minus infinity only, of which alone there is no softmax (its maximum becomes minus infinity then, see packed_to).
 struct PackedRow {
   float m, l, mc;
 };
+constexpr float PACKED_SEES = -3.0e38f, PACKED_SEES_NONE = -3.1e38f;
 __device__ __forceinline__ float packed_mc(float m, float c) { return fmaxf(m * c, -3.0e38f); }
+// limit: keys behind the prefix that the row sees; pre: the prefix's tiles
+__device__ __forceinline__ PackedRow packed_row(const PackedItem &it, int pre, int limit, float c) {
+  const bool sees = it.kt0 < pf_min(it.kt1, pre) || (it.kt1 > pre && limit > (pf_max(it.kt0, pre) - pre) * PF_BK);
+  const float m = sees ? PACKED_SEES : PACKED_SEES_NONE;
+  return {m, 0.0f, packed_mc(m, c)};
+}
 
 // Scores of NKB blocks of 32 keys (accumulators of K Q^T: register i of block kb is key 32 kb + 8 (i / 4) + 4 g + i % 4) -> weights in bf16,
 // the row's state and O moved on.  first: an item's first tile, whose rows have no reference yet.
@@ -417,11 +425,13 @@ struct PackedTo {
   float inv;
   bool past_l2;
 };
+__device__ __forceinline__ float packed_inverse(float sum, bool lost) { return sum > 0.0f ? 1.0f / sum : lost ? __builtin_nanf("") : sum; }   // (a sum that is NaN stays NaN)
 // note: this lane also notes the row's maximum and sum, and with plane 0, of which every parked row has one item, which row of the result it is
 template <int D>
 __device__ __forceinline__ PackedTo<D> packed_to(const PackedParams &P, const PackedItem &it, int row, float2 ml, bool note) {
   const int t = packed_div_group(P, row), h = packed_head(it) * P.group + row - t * P.group, plane = packed_plane(it);
   PackedTo<D> to = {nullptr, nullptr, 1.0f, P.arrivals != nullptr};
+  if (ml.y == 0.0f && ml.x == PACKED_SEES) ml.x = -INFINITY;
   if (plane >= 0) {
     const int id = packed_head(it) * P.head_rows + it.park + row;
     auto put_ml = [&](int p, float2 x) __attribute__((always_inline)) {
@@ -432,12 +442,12 @@ __device__ __forceinline__ PackedTo<D> packed_to(const PackedParams &P, const Pa
     to.part = P.part_o + ((long long)plane * P.part_rows + id) * D;
     if (note) {
       put_ml(plane, ml);
-      for (int i = 1; i <= packed_missing(it); ++i) put_ml(plane + i, make_float2(-3.0e38f, 0.0f));
+      for (int i = 1; i <= packed_missing(it); ++i) put_ml(plane + i, make_float2(PACKED_SEES_NONE, 0.0f));
       if (plane == 0) __hip_atomic_store(P.part_row + id, (it.q_base + t) * P.n_heads + h, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
   } else {
     to.out = P.out + (it.q_base + t) * P.out_tok + h * P.out_head;
-    to.inv = ml.y > 0.0f ? 1.0f / ml.y : ml.y;                    // no key seen: zeros (a sum that is NaN stays NaN)
+    to.inv = packed_inverse(ml.y, ml.x == -INFINITY);
   }
   return to;
 }
@@ -491,7 +501,8 @@ __device__ __forceinline__ void packed_arrive(const PackedItem &it, int32_t *s_l
   const int d0 = tid % LANES * 8;
   for (int r = tid / LANES; r < P.head_rows; r += PACKED_WAVES * 64 / LANES) {
     const int id = head * P.head_rows + r, row = __hip_atomic_load(P.part_row + id, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    float top = -3.0e38f, sum = 0.0f, acc[8] = {};
+    float top = PACKED_SEES_NONE, sum = 0.0f, acc[8] = {};
+    bool lost = false;
     for (int p0 = 0; p0 < P.planes; p0 += AHEAD) {
       float2 ml[AHEAD], x[AHEAD][4];
 #pragma unroll
@@ -503,7 +514,7 @@ __device__ __forceinline__ void packed_arrive(const PackedItem &it, int32_t *s_l
       }
       float new_top = top;
 #pragma unroll
-      for (int i = 0; i < AHEAD; ++i) new_top = fmaxf(new_top, ml[i].x);
+      for (int i = 0; i < AHEAD; ++i) new_top = fmaxf(new_top, ml[i].x), lost |= ml[i].x == -INFINITY;
       const float keep = fast_exp2((top - new_top) * P.scale_log2);
       top = new_top;
       sum *= keep;
@@ -518,7 +529,7 @@ __device__ __forceinline__ void packed_arrive(const PackedItem &it, int32_t *s_l
         for (int e = 0; e < 4; ++e) acc[2 * e] += w * x[i][e].x, acc[2 * e + 1] += w * x[i][e].y;
       }
     }
-    const float inv = sum > 0.0f ? 1.0f / sum : sum;
+    const float inv = packed_inverse(sum, lost);
     bf16x8 w;
 #pragma unroll
     for (int e = 0; e < 8; ++e) w[e] = (__bf16)(acc[e] * inv);
@@ -617,6 +628,7 @@ __device__ __forceinline__ void packed_full(const PackedItem &it, char *smem, in
     limit = packed_limit(P, it, row);
     c = P.scale_log2;
   }
+  PackedRow R = packed_row(it, pre, limit, c);
   // Copies go by runs of whole tiles (of the prefix, of the line's own keys): from tile to tile only one scalar offset moves on, and a ragged last
   // tile goes row by row.  With base and offsets worked out for every tile a prompt of 14040 tokens took 757 us instead of 728.
   __amdgpu_buffer_rsrc_t run_k = __builtin_amdgcn_make_buffer_rsrc(nullptr, 0, 0, 0x00020000u), run_v = run_k;
@@ -676,7 +688,6 @@ __device__ __forceinline__ void packed_full(const PackedItem &it, char *smem, in
   for (int db = 0; db < C::NDB; ++db)
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[db][i] = 0.0f;
-  PackedRow R = {-3.0e38f, 0.0f, packed_mc(-3.0e38f, c)};
   unsigned ak, av;
   packed_lds<D>(smem, smem + C::TENSOR_BYTES, lane, ak, av);
   for (int u = 0; u < n_tiles; ++u) {
@@ -719,13 +730,14 @@ __device__ __forceinline__ void packed_thin(const PackedItem &it, char *smem, fl
   for (int db = 0; db < C::NDB; ++db)
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[db][i] = 0.0f;
-  PackedRow R = {-3.0e38f, 0.0f, packed_mc(-3.0e38f, c)};
+  const int limit = packed_limit(P, it, row);
+  PackedRow R = packed_row(it, K.pre, limit, c);
   if (j0 < j1) {
     bf16x8 qf[C::NKS];
     packed_load_q<D>(P, it, row, g, qf);
     packed_copy<D, false, KEYS>(P, it, K, it.kt0 + j0 / 2, j0 % 2 * KEYS, mine_k, lane);
     packed_copy<D, true, KEYS>(P, it, K, it.kt0 + j0 / 2, j0 % 2 * KEYS, mine_v, lane);
-    const int limit = packed_limit(P, it, row), lim_first = __builtin_amdgcn_readlane(limit, 0);
+    const int lim_first = __builtin_amdgcn_readlane(limit, 0);
 #pragma unroll
     for (int ks = 0; ks < C::NKS; ++ks) asm volatile("" : "+v"(qf[ks]));
     unsigned ak, av;
@@ -755,7 +767,7 @@ __device__ __forceinline__ void packed_thin(const PackedItem &it, char *smem, fl
   __syncthreads();
   for (int e = tid; e < 32 * (D / 8); e += PACKED_WAVES * 64) {
     const int r = e / (D / 8), d0 = (e % (D / 8)) * 8;
-    float2 ml[PACKED_WAVES], all = make_float2(-3.0e38f, 0.0f);
+    float2 ml[PACKED_WAVES], all = make_float2(PACKED_SEES_NONE, 0.0f);
 #pragma unroll
     for (int w = 0; w < PACKED_WAVES; ++w) ml[w] = s_ml[w * 32 + r], all.x = fmaxf(all.x, ml[w].x);
     f32x4 a = {0.0f, 0.0f, 0.0f, 0.0f}, b = a;
@@ -808,10 +820,11 @@ __global__ __launch_bounds__(256) void pf_packed_join_few_kernel(PackedParams P)
   const int d0 = threadIdx.x % LANES * 8, row = P.part_row[id];
   float2 ml[PACKED_FEW_PLANES];
 #pragma unroll
-  for (int p = 0; p < PACKED_FEW_PLANES; ++p) ml[p] = p < P.planes ? P.part_ml[(long long)p * P.part_rows + id] : make_float2(-3.0e38f, 0.0f);
-  float top = ml[0].x, sum = 0.0f, acc[8] = {};
+  for (int p = 0; p < PACKED_FEW_PLANES; ++p) ml[p] = p < P.planes ? P.part_ml[(long long)p * P.part_rows + id] : make_float2(PACKED_SEES_NONE, 0.0f);
+  float top = PACKED_SEES_NONE, sum = 0.0f, acc[8] = {};
+  bool lost = false;
 #pragma unroll
-  for (int p = 1; p < PACKED_FEW_PLANES; ++p) top = fmaxf(top, ml[p].x);
+  for (int p = 0; p < PACKED_FEW_PLANES; ++p) top = fmaxf(top, ml[p].x), lost |= ml[p].x == -INFINITY;
   f32x4 x[PACKED_FEW_PLANES][2];
 #pragma unroll
   for (int p = 0; p < PACKED_FEW_PLANES; ++p) {
@@ -830,7 +843,7 @@ __global__ __launch_bounds__(256) void pf_packed_join_few_kernel(PackedParams P)
     for (int e = 0; e < 4; ++e) acc[e] += w * x[p][0][e], acc[e + 4] += w * x[p][1][e];
   }
   if (!there) return;
-  const float inv = sum > 0.0f ? 1.0f / sum : sum;
+  const float inv = packed_inverse(sum, lost);
   bf16x8 r;
 #pragma unroll
   for (int i = 0; i < 8; ++i) r[i] = (__bf16)(acc[i] * inv);
@@ -849,14 +862,15 @@ __global__ __launch_bounds__(256) void pf_packed_join_kernel(PackedParams P) {
   const bool there = packed_is_there(P);
   const int d0 = lane % LANES * 8, grp = lane / LANES, row = P.part_row[id];
   float2 ml[PACKED_JOIN_BATCHES];
-  float top = -3.0e38f;
+  float top = PACKED_SEES_NONE;
+  bool lost = false;
 #pragma unroll
   for (int b = 0; b < PACKED_JOIN_BATCHES; ++b) {
-    ml[b] = make_float2(-3.0e38f, 0.0f);
+    ml[b] = make_float2(PACKED_SEES_NONE, 0.0f);
     if (b * 64 + lane < P.planes) ml[b] = P.part_ml[(long long)(b * 64 + lane) * P.part_rows + id];
   }
 #pragma unroll
-  for (int b = 0; b < PACKED_JOIN_BATCHES; ++b) top = fmaxf(top, ml[b].x);
+  for (int b = 0; b < PACKED_JOIN_BATCHES; ++b) top = fmaxf(top, ml[b].x), lost |= __ballot(ml[b].x == -INFINITY) != 0;
 #pragma unroll
   for (int step = 1; step < 64; step *= 2) top = fmaxf(top, packed_lane(top, lane ^ step));
   float w[PACKED_JOIN_BATCHES], sum = 0.0f;
@@ -896,7 +910,7 @@ __global__ __launch_bounds__(256) void pf_packed_join_kernel(PackedParams P) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) acc[e] += packed_lane(acc[e], lane ^ step);
   if (grp != 0 || !there) return;
-  const float inv = sum > 0.0f ? 1.0f / sum : sum;
+  const float inv = packed_inverse(sum, lost);
   bf16x8 r;
 #pragma unroll
   for (int i = 0; i < 8; ++i) r[i] = (__bf16)(acc[i] * inv);

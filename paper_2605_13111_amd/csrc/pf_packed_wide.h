@@ -55,6 +55,8 @@ __device__ __forceinline__ void packed_wide(const PackedItem &it, char *smem, in
     limit = packed_limit(P, it, row);
     c = P.scale_log2;
   }
+  PackedRow R = packed_row(it, pre, limit, c);
+  asm volatile("" : "+v"(R.m), "+v"(R.mc));                       // worked out here (put off by the compiler a prompt of 14040 tokens took 700 us, so 696)
   // ---- copies, by runs of whole tiles (see packed_full) ----
   __amdgpu_buffer_rsrc_t run_k = __builtin_amdgcn_make_buffer_rsrc(nullptr, 0, 0, 0x00020000u), run_v = run_k;
   unsigned run_soff = 0, run_tile = 0, run_group = 0, run_vk[NC], run_vv = 0;
@@ -128,7 +130,6 @@ __device__ __forceinline__ void packed_wide(const PackedItem &it, char *smem, in
   for (int db = 0; db < C::NDB; ++db)
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[db][i] = 0.0f;
-  PackedRow R = {-3.0e38f, 0.0f, packed_mc(-3.0e38f, c)};
   unsigned ak, av;
   packed_lds<D>(smem, smem + WIDE_KSTAGES * WIDE_TILE, lane, ak, av);
   if (grp == 1) __builtin_amdgcn_s_barrier();                     // group 1 trails by one phase

@@ -438,6 +438,61 @@ def test_prompts_beside_single_tokens_of_many_keys(lq, lk, P, H, KV, D):
     _case(_cu(lq), _cu(lk), H, KV, D, 1, P, seed=91)
 
 
+def _dead(k, dead):
+    """Keys with a score of minus infinity for queries whose first channel is positive."""
+    k[:, dead, 0] = -float("inf")
+    return k
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("which", ["all", "own", "prefix", "first half"])
+@pytest.mark.parametrize("lq,lk,H,KV,D,P,block", [
+    ([70, 5, 9], [70, 5, 4], 4, 2, 64, 0, 1), ([300, 20], [300, 15], 3, 3, 128, 100, 1), ([1] * 4, [900, 3, 0, 64], 4, 2, 128, 700, 1), ([1], [5000], 4, 1, 64, 0, 1),
+    ([1] * 40, [70] * 40, 8, 2, 64, 3000, 0), ([1], [20001], 40, 1, 128, 0, 1), ([1200], [1200], 0, 0, 128, 0, 1), ([1200], [1100], 0, 0, 128, 200, 300)])
+def test_scores_of_minus_infinity(which, lq, lk, H, KV, D, P, block):
+    """Keys whose score is minus infinity weigh nothing; a row that sees no other has no softmax (NaN), one that sees none at all is zero."""
+    if H == 0:
+        H = KV = _wide(lq, lk, 1, block, P)
+    cu_q, cu_k = _cu(lq), _cu(lk)
+    q, k, v, kp, vp = _tensors(H, KV, D, cu_q[-1], cu_k[-1], P, 97, True)
+    q[..., 0] = q[..., 0].abs() + 0.5
+    dead = torch.ones(cu_k[-1], dtype=torch.bool, device=DEV)
+    if which == "prefix":
+        dead[:] = False
+    if which == "first half":
+        for a, b in zip(cu_k, cu_k[1:]):
+            dead[(a + b) // 2:b] = False
+    dead_p = torch.full((P,), which in ("all", "prefix"), dtype=torch.bool, device=DEV)
+    alive = k.clone(), None if kp is None else kp.clone()
+    k = _dead(k, dead)
+    kp = None if kp is None else _dead(kp, dead_p)
+    out = _run(cu_q, cu_k, q, k, v, block, kp, vp).double()
+    G = H // KV
+    for s in range(len(lq)):
+        place = torch.arange(lq[s], device=DEV) + lk[s] - lq[s]
+        j = torch.arange(lk[s], device=DEV)
+        seen = torch.ones((lq[s], lk[s]), dtype=torch.bool, device=DEV)
+        if block:
+            seen = torch.div(j[None], block, rounding_mode="floor") <= torch.div(place[:, None], block, rounding_mode="floor")
+        seen = torch.cat([torch.ones((lq[s], P), dtype=torch.bool, device=DEV), seen], 1)
+        live = seen & ~torch.cat([dead_p, dead[cu_k[s]:cu_k[s + 1]]])[None]
+        none, lost = ~seen.any(1), seen.any(1) & ~live.any(1)
+        for h in range(H):
+            got = out[h, cu_q[s]:cu_q[s + 1]]
+            assert (got[none] == 0).all() and torch.isnan(got[lost]).all()
+            K, V = alive[0][h // G, cu_k[s]:cu_k[s + 1]].double(), v[h // G, cu_k[s]:cu_k[s + 1]].double()
+            if P:
+                K, V = torch.cat([alive[1][h // G].double(), K]), torch.cat([vp[h // G].double(), V])
+            rest = live.any(1)
+            if not rest.any():
+                continue
+            Q = q[h, cu_q[s]:cu_q[s + 1]].double()[rest]
+            w = torch.softmax(torch.where(live[rest], Q @ K.T * D ** -0.5, -math.inf), 1)
+            d = (Q.abs() @ K.abs().T).amax(1, keepdim=True) * D ** -0.5 * (D + 4) * 2.0 ** -24 + 2.0 ** -20   # as in _definition
+            tol = 2.0 ** -8 * (w @ V).abs() + (w @ V.abs()) * (1 + 2.0 ** -8) * (2.0 ** -8 + 2 * d + K.shape[0] * 2.0 ** -24) + 1e-38
+            assert ((got[rest] - w @ V).abs() <= tol).all()
+
+
 @pytest.mark.gpu
 def test_lengths_that_change_need_a_plan():
     """The lengths of a batch written over in place: refused until planned again, right afterwards."""
