@@ -434,7 +434,6 @@ class Packed:
         assert len(cu_q) == len(cu_k) and len(cu_q) >= 2
         n = len(cu_q)
         self.cu_q, self.cu_k = (ctypes.c_int32 * n)(*cu_q), (ctypes.c_int32 * n)(*cu_k)
-        self.total_q, self.total_k = cu_q[-1], cu_k[-1]
         self.n_heads, self.n_kv_heads, self.D, self.prefix_tokens, self.device = int(n_heads), int(n_kv_heads), int(head_dim), int(prefix_tokens), torch.device(device)
         I = ctypes.POINTER(ctypes.c_int32)
         self.c = pf_packed(n - 1, self.n_heads, self.n_kv_heads, self.D, int(block), self.prefix_tokens, 0, 0, 0, -1, -1, 0,
@@ -444,6 +443,10 @@ class Packed:
             raise PfError(PF_ERR_UNSUPPORTED if self.D not in (64, 128) else PF_ERR_INVALID_ARG, "pf_packed_work_bytes")
         self.work = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
         self.c.work, self.c.work_bytes = self.work.data_ptr(), nbytes
+
+    # tokens of the batch as its lengths are now
+    total_q = property(lambda self: self.cu_q[len(self.cu_q) - 1])
+    total_k = property(lambda self: self.cu_k[len(self.cu_k) - 1])
 
 
 def pf_packed_plan(packed, stream=None):

@@ -152,6 +152,15 @@ def test_tensors_of_another_device_are_refused():
         B.pf_packed_plan(B.Packed([0, 4], [0, 4], 2, 2, 64, device="cpu"))
 
 
+def test_totals_follow_the_lengths():
+    """Lengths that are written over in place are the batch's lengths, for a caller who sizes tensors by them too."""
+    packed = B.Packed([0, 4, 9], [0, 5, 12], 2, 2, 64, device="cpu")
+    assert (packed.total_q, packed.total_k) == (9, 12)
+    packed.cu_k[1], packed.cu_k[2] = 6, 14
+    packed.cu_q[2] = 8
+    assert (packed.total_q, packed.total_k) == (8, 14)
+
+
 # ---- results ----------------------------------------------------------------------------------------------------------
 
 def _definition(q, k, v, cu_q, cu_k, block, kp=None, vp=None, scale=None):
