@@ -432,6 +432,8 @@ class Packed:
     def __init__(self, cu_q, cu_k, n_heads, n_kv_heads, head_dim, block=1, prefix_tokens=0, device="cuda:0"):
         cu_q, cu_k = [int(x) for x in cu_q], [int(x) for x in cu_k]
         assert len(cu_q) == len(cu_k) and len(cu_q) >= 2
+        if any(not -2 ** 31 <= x < 2 ** 31 for x in (*cu_q, *cu_k, int(n_heads), int(n_kv_heads), int(head_dim), int(block), int(prefix_tokens))):
+            raise PfError(PF_ERR_INVALID_ARG, "Packed")           # ctypes would cut them down to the struct's 32 bits
         n = len(cu_q)
         self.cu_q, self.cu_k = (ctypes.c_int32 * n)(*cu_q), (ctypes.c_int32 * n)(*cu_k)
         self.n_heads, self.n_kv_heads, self.D, self.prefix_tokens, self.device = int(n_heads), int(n_kv_heads), int(head_dim), int(prefix_tokens), torch.device(device)

@@ -161,6 +161,16 @@ def test_totals_follow_the_lengths():
     assert (packed.total_q, packed.total_k) == (8, 14)
 
 
+@pytest.mark.parametrize("kw", [dict(cu_q=[0, 2 ** 32 + 5]), dict(cu_k=[0, 2 ** 32 + 5]), dict(block=2 ** 32), dict(prefix_tokens=2 ** 32), dict(n_heads=2 ** 32 + 2)])
+def test_numbers_beyond_32_bits_are_refused(kw):
+    """Cut down to the struct's 32 bits, each of these would be another batch: fewer tokens, no mask, no prefix."""
+    args = dict(cu_q=[0, 5], cu_k=[0, 5], n_heads=2, n_kv_heads=2, head_dim=64)
+    B.Packed(**args, device="cpu")
+    with pytest.raises(B.PfError) as e:
+        B.Packed(**{**args, **kw}, device="cpu")
+    assert e.value.status == B.PF_ERR_INVALID_ARG
+
+
 # ---- results ----------------------------------------------------------------------------------------------------------
 
 def _definition(q, k, v, cu_q, cu_k, block, kp=None, vp=None, scale=None):
