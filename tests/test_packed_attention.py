@@ -512,6 +512,60 @@ def test_scores_of_minus_infinity(which, lq, lk, H, KV, D, P, block):
             assert ((got[rest] - w @ V).abs() <= tol).all()
 
 
+def _tile_channels(cu_k, KV, D, P, device):
+    """Values that say which tile of 64 keys they are from: key j of tile t (the prefix's tiles, then the sequence's own) has a value in channel t % D
+    only.  A tile left out takes its share of one channel, whatever the length."""
+    def values(tile):
+        v = torch.zeros((tile.shape[0], KV, D), dtype=torch.bfloat16)
+        v[torch.arange(tile.shape[0]), :, tile % D] = 1.0
+        return v.to(device).transpose(0, 1)
+    pre = (P + 63) // 64
+    own = torch.cat([pre + torch.arange(b - a) // 64 for a, b in zip(cu_k, cu_k[1:])])
+    return values(own), values(torch.arange(P) // 64) if P else None
+
+
+LONG = [([1], [20000], 8, 1, 0), ([1], [40001], 40, 1, 0), ([1], [65536], 8, 8, 0), ([1] * 3, [9000, 130, 20001], 4, 4, 9000), ([1] * 40, [70] * 40, 8, 2, 20000),
+        ([5, 1, 2], [30000, 9, 64], 2, 2, 5000), ([900, 1, 1], [900, 30000, 12000], 4, 2, 0)]
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_a_lost_tile_would_be_seen(D):
+    """The bound that results are held to is passed twice over by any one tile of 64 keys left out of the definition, at the longest of these lengths."""
+    n = 65536
+    g = torch.Generator().manual_seed(5)
+    q, k = torch.randn((1, 1, D), generator=g).to(torch.bfloat16), torch.randn((1, n, D), generator=g).to(torch.bfloat16)
+    v, _ = _tile_channels([0, n], 1, D, 0, "cpu")
+    want, tol = _definition(q, k, v, [0, 1], [0, n], 1)
+    w = torch.softmax(k[0].double() @ q[0, 0].double() * D ** -0.5, 0).view(-1, 64).sum(1)
+    channel = torch.arange(n // 64) % D
+    share = want[0, 0, channel]
+    without = (share - w) / (1 - w)                               # the tile's channel once the tile is lost, the other weights' sum taken as all
+    assert ((share - without) > 2 * tol[0, 0, channel]).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("lq,lk,H,KV,P", LONG)
+@pytest.mark.parametrize("D", [64, 128])
+def test_every_tile_counts(lq, lk, H, KV, P, D):
+    cu_q, cu_k = _cu(lq), _cu(lk)
+    q, k, _, kp, _ = _tensors(H, KV, D, cu_q[-1], cu_k[-1], P, 57, True)
+    v, vp = _tile_channels(cu_k, KV, D, P, DEV)
+    out = _run(cu_q, cu_k, q, k, v, 1, kp, vp)
+    want, tol = _definition(q, k, v, cu_q, cu_k, 1, kp, vp)
+    assert torch.isfinite(out).all() and ((out.double() - want).abs() <= tol).all()
+
+
+@pytest.mark.gpu
+def test_every_tile_counts_in_wide_items():
+    lq, D = [4801, 130], 128
+    KV, cu = _wide(lq, lq, 1, 1), _cu(lq)
+    q, k, _, _, _ = _tensors(KV, KV, D, cu[-1], cu[-1], 0, 57, True)
+    v, _ = _tile_channels(cu, KV, D, 0, DEV)
+    out = _run(cu, cu, q, k, v, 1)
+    want, tol = _definition(q, k, v, cu, cu, 1)
+    assert torch.isfinite(out).all() and ((out.double() - want).abs() <= tol).all()
+
+
 @pytest.mark.gpu
 def test_lengths_that_change_need_a_plan():
     """The lengths of a batch written over in place: refused until planned again, right afterwards."""
