@@ -452,7 +452,7 @@ class Packed:
 
 
 def pf_packed_plan(packed, stream=None):
-    assert packed.work.get_device() == _current_device()
+    assert packed.work.get_device() == _current_device() and packed.work.data_ptr() == packed.c.work
     _check(lib().pf_packed_plan(ctypes.byref(packed.c), _stream(stream)), "pf_packed_plan")
 
 
@@ -484,7 +484,7 @@ def pf_packed_attn_fwd(packed, q, k, v, out, workspace, k_prefix=None, v_prefix=
     if workspace is not None:
         assert workspace.get_device() == dev and workspace.is_contiguous()
         ws, ws_bytes = workspace.data_ptr(), workspace.nbytes
-    assert packed.work.get_device() == dev
+    assert packed.work.get_device() == dev and packed.work.data_ptr() == c.work
     rc = (_lib or lib()).pf_packed_attn_fwd(ctypes.byref(c), q.data_ptr(), _packed_layout(H, tq, D, dev, q), k.data_ptr(), v.data_ptr(),
                                             _packed_layout(KV, c.total_k, D, dev, k, v), kp, vp, pl, out.data_ptr(),
                                             _packed_layout(H, tq, D, dev, out), softmax_scale, ws, ws_bytes, _raw_stream(dev) if stream is None else stream)

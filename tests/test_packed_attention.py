@@ -319,6 +319,24 @@ def test_host_tensors_are_refused():
 
 
 @pytest.mark.gpu
+def test_a_buffer_replaced_beside_the_struct_is_refused():
+    """The struct holds an address; the tensor that it belongs to has to be the batch's still."""
+    cu = [0, 7]
+    q, k, v, _, _ = _tensors(2, 2, 64, 7, 7, 0, 1, True)
+    packed = B.Packed(cu, cu, 2, 2, 64, device=DEV)
+    B.pf_packed_plan(packed)
+    ws, out, kept = torch.empty(B.pf_packed_workspace_bytes(packed), dtype=torch.uint8, device=DEV), torch.empty_like(q), packed.work
+    packed.work = torch.zeros_like(kept)
+    with pytest.raises(AssertionError):
+        B.pf_packed_attn_fwd(packed, q, k, v, out, ws)
+    with pytest.raises(AssertionError):
+        B.pf_packed_plan(packed)
+    packed.work = kept
+    B.pf_packed_attn_fwd(packed, q, k, v, out, ws)
+    assert torch.isfinite(out).all()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("P", [0, 100])
 def test_rows_behind_the_last_sequence(D, P):
