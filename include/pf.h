@@ -343,7 +343,8 @@ int pf_rope_init(pf_rope *rope, int head_dim, int rot_dim, int interleaved, int 
 /* One tensor of pf_qk_norm_rope: rows of n_heads heads per token. */
 typedef struct pf_rope_rows {
   const void *x;               /* dev bf16, 16-byte aligned */
-  void *out;                   /* dev bf16, 16-byte aligned; may be x with the same layout, must not overlap x otherwise */
+  void *out;                   /* dev bf16, 16-byte aligned; may be x with the same layout, must not overlap x otherwise, nor
+                                  the other tensor's x or out */
   const void *weight;          /* dev bf16 [head_dim], 16-byte aligned, or NULL (= 1) */
   int32_t n_heads;             /* 0 = this tensor is left out (all pointers NULL) */
   int32_t reserved;            /* must be 0 */

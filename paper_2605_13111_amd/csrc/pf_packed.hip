@@ -18,9 +18,9 @@
 // (pf_packed_wide.h): 256 rows, eight waves that alternate between matrix and vector work, one workgroup per compute unit; a whole batch is
 // laid out with one or the other, whichever the planner finds faster (one head_dim-128 prompt of 16 heads: 1200 tokens 24 us either way,
 // 4800 tokens 109 full and 101 wide, 9600 tokens 340 and 319).  Thin: at most 32 rows, among the full ones.
-// Bound: prompts by the matrix pipe and the power it may draw (14040 tokens of 12 heads 1210 TFLOP/s, where a plain product of 8192^3 reaches
-// 1214; head_dim 64 by the vector ALU too: 966), single tokens by HBM (64 answers behind 16384 tokens: 4.6 TB/s, a plain copy 4.9), short
-// launches by what an item costs whatever its length: some 3 us to its first tile and 1.5 for its results.
+// Bound: prompts by the matrix pipe and the power it may draw (14040 tokens of 12 heads 1130 to 1210 TFLOP/s, 666 to 712 us from card to card,
+// where a plain product of 8192^3 reached 1214; head_dim 64 by the vector ALU too: 910 to 966), single tokens by HBM (64 answers behind 16384
+// tokens: 4.6 TB/s, a plain copy 4.9), short launches by what an item costs whatever its length: some 3 us to its first tile and 1.5 for its results.
 //
 // Scores, softmax and value products as in the ragged-cache kernels: S^T = K Q^T and O^T += V^T P^T on 32x32x16 bf16 MFMAs with fp32
 // accumulation, one query row per lane; weights are rounded to bf16 for the second product (2^-8 relative at most each, the sum is
@@ -407,7 +407,8 @@ __device__ __forceinline__ void packed_read_q(const char *stage, int lane, bf16x
   }
 }
 // Partial results that the head's last workgroup joins cross workgroups on different dies, each with an L2 of its own: they are written and read
-// at device scope, 8 bytes at a time, past the L2; the wait for the stores before the arrival is all that stands between.
+// at device scope, 8 bytes at a time, past the L2; the wait for the stores before the arrival is all that stands between.  With the memory model's
+// own fences (PF_STRICT_FENCES), which write back and drop whole L2s, one row of 12 heads behind 4096 keys takes 13.9 us and not 10.6.
 __device__ __forceinline__ void packed_st8(void *p, float a, float b) {
   __hip_atomic_store((unsigned long long *)p, (unsigned long long)__float_as_uint(a) | (unsigned long long)__float_as_uint(b) << 32, __ATOMIC_RELAXED,
                      __HIP_MEMORY_SCOPE_AGENT);

@@ -9,9 +9,9 @@
 //   vector phase u   sends the copies of tile u + 3 to where tiles u - 1 (K) and u - 2 (V) were (their last readers, both groups' matrix phases
 //                    u - 1, are two barriers back), then scores of tile u -> weights
 // Bound: both kinds of phase (1260 cycles of the 992 that 31 MFMAs take: vector instructions of the other wave hold their issue up; 960 of
-// weights and 255 of copies), at the clock that the power leaves (1.7 GHz).  A prompt of 14040 tokens of 12 heads takes 666 us (1210 TFLOP/s), as
-// 128-row items, two workgroups per compute unit, 741: there a key tile is copied into LDS twice for 256 rows, and the matrix pipe waits for
-// softmaxes.  Not better, each measured on that prompt at 700: copies sent between the MFMAs (744), the barrier 3, 4 or 6 MFMAs early (757, 764,
+// weights and 255 of copies), at the clock that the power leaves (1.7 GHz).  A prompt of 14040 tokens of 12 heads takes 666 to 712 us from card to
+// card (1210 to 1130 TFLOP/s); as 128-row items, two workgroups per compute unit, it took 741 when this form took 695: there a key tile is copied
+// into LDS twice for 256 rows, and the matrix pipe waits for softmaxes.  Not better, each measured on that prompt at 700: copies sent between the MFMAs (744), the barrier 3, 4 or 6 MFMAs early (757, 764,
 // 782; 2: the same), matrix phases without priority (713).  Workgroups that stay resident and take items, with the copies of the next one under
 // way: 740 from lists made beforehand (the dies do not run at one speed), 713 by tickets.
 #ifndef PF_PACKED_WIDE_H

@@ -10,7 +10,8 @@
 // Bound: HBM, every row is read and written once.  A wave takes one token (or some of its heads, where tokens are few): its lanes work
 // the token's cosines and sines out once, one pair each, and all heads of the token share them; a row is D / 8 lanes wide, and a
 // lane holds whole pairs in either layout (eight neighbouring channels, or four of each half), so that nothing crosses lanes but the sum of squares.
-// 88920 tokens of 24 heads of 128: 190 us, 5.7 TB/s read and written (a plain copy: 4.9).
+// 88920 tokens of 24 heads of 128: 190 us, 5.7 TB/s read and written; torch's copy of the same bytes takes 203, this kernel without norm and
+// rotation 199 and with the rotation alone 185, so the vector ALU, which its counters show as busy all the time, does not bind.
 #include <math.h>
 #include <type_traits>
 #include "pf_internal.h"
